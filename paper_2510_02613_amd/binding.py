@@ -29,6 +29,9 @@ EXPORTS = ("moe_workspace_bytes", "moe_layer_create", "moe_set_expert_map", "moe
            "moe_vpool_map", "moe_vpool_unmap", "moe_vpool_page_of", "moe_vpool_destroy", "moe_vpool_slot_bytes",
            "moe_vpool_slots", "moe_layer_bind_vpools", "moe_ceiling_tile_stream", "moe_profile_select", "moe_forward_static",
            "moe_pool_export", "moe_pool_open", "moe_pool_close")
+# and include/elasticmoe_scaled.h
+EXPORTS_SCALED = ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu", "moe_scaled_swiglu_workspace_bytes",
+                  "moe_scaled_workspace_bytes", "moe_layer_create_scaled", "moe_load_expert_scaled", "moe_forward_scaled")
 MOE_IPC_HANDLE_BYTES = 64
 MOE_STATIC_SCRATCH_BYTES = 32 << 20
 MOE_N_PHASES = 5
@@ -53,6 +56,35 @@ class MoEWorkspaceView(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("topk_ids", "topk_w", "counts", "offsets", "perm", "inv", "h", "y", "active_map", "tiles", "n_tiles",
                  "unit_hdr", "units0", "units1")]
+
+
+class MoERmsNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("ld_sum", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("q_scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64)]
+
+
+class MoEQuantize(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("block_rows", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64)]
+
+
+class MoEScaledMatmul(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("ld_a", ctypes.c_int64), ("a_scale", ctypes.c_void_p), ("ld_a_scale", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p), ("add", ctypes.c_void_p), ("ld_add", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64)]
+
+
+class MoEScaledSwiglu(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int32), ("inter", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("ld_a", ctypes.c_int64), ("a_scale", ctypes.c_void_p), ("ld_a_scale", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("q_scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 class MoEError(RuntimeError):
@@ -142,6 +174,23 @@ def lib() -> ctypes.CDLL:
         L.moe_ceiling_stream.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
         L.moe_ceiling_tile_stream.restype = ctypes.c_int
         L.moe_ceiling_tile_stream.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p]
+        for name, args in (("moe_rms_norm", MoERmsNorm), ("moe_quantize", MoEQuantize),
+                           ("moe_scaled_matmul", MoEScaledMatmul), ("moe_scaled_swiglu", MoEScaledSwiglu)):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+        L.moe_scaled_workspace_bytes.restype = ctypes.c_size_t
+        L.moe_scaled_workspace_bytes.argtypes = [ctypes.POINTER(MoEConfig)]
+        L.moe_layer_create_scaled.restype = ctypes.c_int
+        L.moe_layer_create_scaled.argtypes = [ctypes.POINTER(MoEConfig), ctypes.POINTER(MoEBuffers), ctypes.c_void_p, ctypes.c_void_p,
+                                              ctypes.POINTER(ctypes.c_void_p)]
+        L.moe_load_expert_scaled.restype = ctypes.c_int
+        L.moe_load_expert_scaled.argtypes = [ctypes.c_void_p, ctypes.c_int32] + [ctypes.c_void_p] * 6 + [ctypes.c_int32]
+        L.moe_forward_scaled.restype = ctypes.c_int
+        L.moe_forward_scaled.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_uint32]
+        L.moe_scaled_swiglu_workspace_bytes.restype = ctypes.c_size_t
+        L.moe_scaled_swiglu_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
         L.moe_last_error.restype = ctypes.c_char_p
         L.moe_last_error.argtypes = []
         _lib = L
@@ -342,6 +391,51 @@ def moe_ceiling_tile_stream(buf_ptr: int, n_tiles: int, row_bytes: int, non_temp
     """Enqueue one read of n_tiles tiles of 256 rows x row_bytes in the access shape of the large-tile kernels' weight loaders."""
     _check(lib().moe_ceiling_tile_stream(ctypes.c_void_p(buf_ptr), ctypes.c_int32(n_tiles), ctypes.c_size_t(row_bytes),
                                          ctypes.c_int32(int(non_temporal)), ctypes.c_void_p(stream)))
+
+
+def moe_scaled_workspace_bytes(cfg: MoEConfig) -> int:
+    n = lib().moe_scaled_workspace_bytes(ctypes.byref(cfg))
+    if n == 0:
+        raise MoEError(MOE_ERR_SHAPE, moe_last_error())
+    return int(n)
+
+
+def moe_layer_create_scaled(cfg: MoEConfig, buf: MoEBuffers, w13_scale_ptr: int, w2_scale_ptr: int) -> ctypes.c_void_p:
+    h = ctypes.c_void_p()
+    _check(lib().moe_layer_create_scaled(ctypes.byref(cfg), ctypes.byref(buf), w13_scale_ptr, w2_scale_ptr, ctypes.byref(h)))
+    return h
+
+
+def moe_load_expert_scaled(layer, slot: int, src_w13_ptr: int, src_w13_scale_ptr: int, src_w2_ptr: int, src_w2_scale_ptr: int,
+                           copy_stream: int, serve_stream: int, copy_blocks: int = 0) -> None:
+    _check(lib().moe_load_expert_scaled(layer, slot, src_w13_ptr, src_w13_scale_ptr, src_w2_ptr, src_w2_scale_ptr,
+                                        copy_stream, serve_stream, copy_blocks))
+
+
+def moe_forward_scaled(layer, x_ptr: int, xq_ptr: int, x_scale_ptr: int, T: int, ids_ptr: int, w_ptr: int, out_ptr: int,
+                       shared_begin: int = 0, shared_end: int = 0, stream: int = 0, flags: int = 0) -> None:
+    _check(lib().moe_forward_scaled(layer, x_ptr, xq_ptr, x_scale_ptr, T, ids_ptr, w_ptr, shared_begin, shared_end, out_ptr,
+                                    stream, flags))
+
+
+def moe_rms_norm(args: MoERmsNorm, stream: int = 0) -> None:
+    _check(lib().moe_rms_norm(args, stream))
+
+
+def moe_quantize(args: MoEQuantize, stream: int = 0) -> None:
+    _check(lib().moe_quantize(args, stream))
+
+
+def moe_scaled_matmul(args: MoEScaledMatmul, stream: int = 0) -> None:
+    _check(lib().moe_scaled_matmul(args, stream))
+
+
+def moe_scaled_swiglu_workspace_bytes(m: int, inter: int, k: int) -> int:
+    return int(lib().moe_scaled_swiglu_workspace_bytes(m, inter, k))
+
+
+def moe_scaled_swiglu(args: MoEScaledSwiglu, stream: int = 0) -> None:
+    _check(lib().moe_scaled_swiglu(args, stream))
 
 
 def moe_layer_destroy(layer) -> None:

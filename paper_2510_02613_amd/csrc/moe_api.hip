@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "moe_internal.h"
+#include "scaled.h"
 
 using namespace emoe;
 
@@ -55,13 +56,14 @@ constexpr int kMinTileRows = 16;  // smallest M-tile any expert kernel uses: siz
 // Offsets of every intermediate inside the workspace.
 struct Layout {
     size_t map, logits, ids, w, slot_rank, blk_hist, blk_cnt, counts, offs, perm, inv, tiles, n_tiles, units[2], unit_hdr, h, y, partials, total;
+    size_t xq, xs, hq, hs;   // layers with 8-bit experts: the tokens and the rows of h in 8 bits, their scales (h itself: fp32 rows)
     size_t unit_cap, logit_tokens;
     bool has_partials;
 };
 
 size_t esize(int dtype) { return dtype == MOE_BF16 ? 2 : 4; }
 
-moe_status_t check_config(const moe_config_t *c)
+moe_status_t check_config(const moe_config_t *c, bool scaled = false)
 {
     if (!c) return fail(MOE_ERR_ARG, "config is NULL");
     if (c->hidden <= 0 || c->inter <= 0 || c->n_experts <= 0 || c->top_k <= 0 || c->n_slots <= 0 || c->max_tokens <= 0)
@@ -87,13 +89,19 @@ moe_status_t check_config(const moe_config_t *c)
     if (c->n_slots > 2047) return fail(MOE_ERR_UNSUPPORTED, "n_slots > 2047");
     if ((long long)c->max_tokens * (c->top_k + c->n_shared) > (1ll << 26))
         return fail(MOE_ERR_UNSUPPORTED, "max_tokens * (top_k + n_shared) > 2^26");
+    if (scaled) {
+        if (c->act_dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "8-bit experts take bf16 activations");
+        if (c->hidden % 16 || c->inter % 16) return fail(MOE_ERR_UNSUPPORTED, "hidden and inter must be multiples of 16 (16-byte rows of 8-bit values)");
+        if (c->hidden > kMaxRowCols || c->inter > kMaxRowCols) return fail(MOE_ERR_UNSUPPORTED, "hidden or inter > %d", kMaxRowCols);
+        if ((long long)c->max_tokens * (c->top_k + c->n_shared) > (1ll << 21)) return fail(MOE_ERR_UNSUPPORTED, "max_tokens * (top_k + n_shared) > 2^21");
+    }
     return MOE_OK;
 }
 
 // tight: where the size is fixed and the pass would not fit otherwise (moe_forward_static) -- the logits of an fp32
 // layer share the memory of what is written after the selection has read them, as many tokens at a time as that
 // holds, and the large-tile GEMMs serve small groups no more (no unit lists)
-Layout make_layout(const moe_config_t &c, bool tight = false)
+Layout make_layout(const moe_config_t &c, bool tight = false, bool scaled = false)
 {
     Layout L;
     const size_t T = c.max_tokens, k = c.top_k, kk = c.top_k + c.n_shared, S = c.n_slots;
@@ -130,7 +138,7 @@ Layout make_layout(const moe_config_t &c, bool tight = false)
     L.n_tiles = take(4);
     // unit lists of the large-tile GEMMs (layers they can serve): one entry per (tile, run of N-slices), in rows of 8
     L.unit_cap = 0;
-    if (c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (!tight || A >= 48 * S)) {
+    if (!scaled && c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (!tight || A >= 48 * S)) {
         const size_t big_tiles = (A + mfma8_tile_rows() - 1) / mfma8_tile_rows() + S;
         const int ns0 = mfma8_n_slices(c.hidden, c.inter, 0), ns1 = mfma8_n_slices(c.hidden, c.inter, 1);
         L.unit_cap = 8 * (size_t)mfma8_grid_rows((int)big_tiles, ns0 > ns1 ? ns0 : ns1);
@@ -138,10 +146,14 @@ Layout make_layout(const moe_config_t &c, bool tight = false)
     L.units[0] = take(sizeof(MUnit) * L.unit_cap);
     L.units[1] = take(sizeof(MUnit) * L.unit_cap);
     L.unit_hdr = take(L.unit_cap ? 2 * sizeof(UnitHdr) : 0);
-    L.h = take(esize(c.act_dtype) * A * c.inter);
+    L.h = take((scaled ? 4 : esize(c.act_dtype)) * A * c.inter);
+    L.xq = take(scaled ? T * c.hidden : 0);
+    L.xs = take(scaled ? 4 * T * scale_blocks(c.hidden) : 0);
+    L.hq = take(scaled ? A * c.inter : 0);
+    L.hs = take(scaled ? 4 * A * scale_blocks(c.inter) : 0);
     L.y = take(esize(c.act_dtype) * A * c.hidden);
     // partial sums of split tiles: only layers whose large-tile GEMMs can have contractions long enough to split
-    L.has_partials = c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (c.hidden >= 4096 || c.inter >= 4096) &&
+    L.has_partials = !scaled && c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (c.hidden >= 4096 || c.inter >= 4096) &&
                      A >= 48 * S;
     L.partials = take(L.has_partials ? mfma8_partial_bytes() : 0);
     if (shared_logits) {
@@ -167,6 +179,9 @@ struct moe_layer {
     hipEvent_t ev[kProfRing][MOE_N_PHASES + 1] = {};
     moe_config_t cfg;
     moe_buffers_t buf;
+    const float *w13_scale = nullptr, *w2_scale = nullptr;   // 8-bit experts: w13 and w2 are e4m3 pools with these scales
+    bool scaled() const { return w13_scale != nullptr; }
+    size_t weight_bytes() const { return scaled() ? 1 : esize(cfg.act_dtype); }   // of one weight
     Layout lay;
     bool has_map;
     std::vector<int32_t> slot_owner;  // per slot: entry (expert, or E + shared expert) of the active table that uses it, or -1
@@ -221,11 +236,17 @@ size_t moe_workspace_bytes(const moe_config_t *cfg)
     return make_layout(*cfg).total;
 }
 
-moe_status_t moe_layer_create(const moe_config_t *cfg, const moe_buffers_t *buf, moe_layer_t **out)
+size_t moe_scaled_workspace_bytes(const moe_config_t *cfg)
+{
+    if (check_config(cfg, true) != MOE_OK) return 0;
+    return make_layout(*cfg, false, true).total;
+}
+
+static moe_status_t create_layer(const moe_config_t *cfg, const moe_buffers_t *buf, bool scaled, const float *w13_scale, const float *w2_scale, moe_layer_t **out)
 {
     if (!out) return fail(MOE_ERR_ARG, "out is NULL");
     *out = nullptr;
-    moe_status_t st = check_config(cfg);
+    moe_status_t st = check_config(cfg, scaled);
     if (st != MOE_OK) return st;
     if (!buf) return fail(MOE_ERR_ARG, "buffers is NULL");
     if (!buf->router_w || !buf->w13 || !buf->w2 || !buf->workspace)
@@ -235,17 +256,32 @@ moe_status_t moe_layer_create(const moe_config_t *cfg, const moe_buffers_t *buf,
     if (!aligned(buf->workspace, kAlign)) return fail(MOE_ERR_ARG, "workspace must be 256-byte aligned");
     if ((buf->logit_bias && !aligned(buf->logit_bias, 4)) || (buf->select_bias && !aligned(buf->select_bias, 4)))
         return fail(MOE_ERR_ARG, "bias vectors must be 4-byte aligned");
-    Layout L = make_layout(*cfg);
+    if (scaled) {
+        if (!w13_scale || !w2_scale) return fail(MOE_ERR_ARG, "w13_scale and w2_scale must be non-NULL");
+        if (!aligned(w13_scale, 4) || !aligned(w2_scale, 4)) return fail(MOE_ERR_ARG, "w13_scale and w2_scale must be 4-byte aligned");
+    }
+    Layout L = make_layout(*cfg, false, scaled);
     if (buf->workspace_bytes < L.total)
         return fail(MOE_ERR_CAPACITY, "workspace has %zu bytes, layer needs %zu", buf->workspace_bytes, L.total);
     moe_layer *l = new (std::nothrow) moe_layer;
     if (!l) return fail(MOE_ERR_ARG, "out of host memory");
     l->cfg = *cfg;
     l->buf = *buf;
+    if (scaled) { l->w13_scale = w13_scale; l->w2_scale = w2_scale; }
     l->lay = L;
     l->has_map = false;
     *out = l;
     return MOE_OK;
+}
+
+moe_status_t moe_layer_create(const moe_config_t *cfg, const moe_buffers_t *buf, moe_layer_t **out)
+{
+    return create_layer(cfg, buf, false, nullptr, nullptr, out);
+}
+
+moe_status_t moe_layer_create_scaled(const moe_config_t *cfg, const moe_buffers_t *buf, const float *w13_scale, const float *w2_scale, moe_layer_t **out)
+{
+    return create_layer(cfg, buf, true, w13_scale, w2_scale, out);
 }
 
 moe_status_t moe_ceiling_mfma(int32_t blocks, int32_t iters, int32_t random_operands, float *sink, void *hip_stream, double *flops)
@@ -483,7 +519,7 @@ moe_status_t moe_layer_bind_vpools(moe_layer_t *l, moe_vpool_t *w13_pool, moe_vp
 {
     if (!l) return fail(MOE_ERR_ARG, "layer is NULL");
     const moe_config_t &c = l->cfg;
-    const size_t es = esize(c.act_dtype);
+    const size_t es = l->weight_bytes();
     const size_t want[2] = {2 * (size_t)c.inter * c.hidden * es, (size_t)c.hidden * c.inter * es};
     moe_vpool_t *pool[2] = {w13_pool, w2_pool};
     const void *base[2] = {l->buf.w13, l->buf.w2};
@@ -531,10 +567,10 @@ static bool serve_pending(moe_layer *l, hipStream_t serve, hipStream_t copy)
     return q != hipSuccess;
 }
 
-moe_status_t moe_load_expert(moe_layer_t *l, int32_t slot, const void *src_w13, const void *src_w2,
-                             void *copy_stream, void *serve_stream, int32_t copy_blocks)
+// src_s13, src_s2: the scales of 8-bit weights (a layer that has such), else NULL
+static moe_status_t fill_slot(moe_layer_t *l, int32_t slot, const void *src_w13, const float *src_s13, const void *src_w2, const float *src_s2,
+                              void *copy_stream, void *serve_stream, int32_t copy_blocks)
 {
-    if (!l) return fail(MOE_ERR_ARG, "layer is NULL");
     const moe_config_t &c = l->cfg;
     if (slot < 0 || slot >= c.n_slots) return fail(MOE_ERR_ARG, "slot %d is outside [0, %d)", slot, c.n_slots);
     if (!src_w13 || !src_w2) return fail(MOE_ERR_ARG, "src_w13 and src_w2 must be non-NULL");
@@ -563,11 +599,16 @@ moe_status_t moe_load_expert(moe_layer_t *l, int32_t slot, const void *src_w13, 
         e = hipEventRecord(l->serve_ev, (hipStream_t)serve_stream);
         if (e == hipSuccess) e = hipStreamWaitEvent((hipStream_t)copy_stream, l->serve_ev, 0);
     }
-    const size_t es = esize(c.act_dtype);
+    const size_t es = l->weight_bytes();
     const size_t b13 = 2 * (size_t)c.inter * c.hidden * es, b2 = (size_t)c.hidden * c.inter * es;
     if (e == hipSuccess)
         e = launch_fill_slot((char *)const_cast<void *>(l->buf.w13) + (size_t)slot * b13, src_w13, b13,
                              (char *)const_cast<void *>(l->buf.w2) + (size_t)slot * b2, src_w2, b2, copy_blocks, (hipStream_t)copy_stream);
+    if (e == hipSuccess && l->scaled()) {
+        const size_t n13 = 2 * (size_t)scale_blocks(c.inter) * scale_blocks(c.hidden), n2 = n13 / 2;
+        e = launch_fill_scales(const_cast<float *>(l->w13_scale) + (size_t)slot * n13, src_s13, n13, const_cast<float *>(l->w2_scale) + (size_t)slot * n2, src_s2, n2,
+                               (hipStream_t)copy_stream);
+    }
     // the event is about to stand for this fill alone: the one it stood for comes first.  (On one stream it does
     // anyway; a handle can also name another stream by now, a destroyed one's successor or another thread's own.)
     if (e == hipSuccess && at < l->n_pending) e = hipStreamWaitEvent((hipStream_t)copy_stream, l->load_ev[at].ev, 0);
@@ -576,6 +617,24 @@ moe_status_t moe_load_expert(moe_layer_t *l, int32_t slot, const void *src_w13, 
     l->load_ev[at].stream = copy_stream;
     if (at == l->n_pending) l->n_pending++;
     return MOE_OK;
+}
+
+moe_status_t moe_load_expert(moe_layer_t *l, int32_t slot, const void *src_w13, const void *src_w2,
+                             void *copy_stream, void *serve_stream, int32_t copy_blocks)
+{
+    if (!l) return fail(MOE_ERR_ARG, "layer is NULL");
+    if (l->scaled()) return fail(MOE_ERR_UNSUPPORTED, "this layer's experts have scales: use moe_load_expert_scaled");
+    return fill_slot(l, slot, src_w13, nullptr, src_w2, nullptr, copy_stream, serve_stream, copy_blocks);
+}
+
+moe_status_t moe_load_expert_scaled(moe_layer_t *l, int32_t slot, const void *src_w13, const float *src_w13_scale, const void *src_w2, const float *src_w2_scale,
+                                    void *copy_stream, void *serve_stream, int32_t copy_blocks)
+{
+    if (!l) return fail(MOE_ERR_ARG, "layer is NULL");
+    if (!l->scaled()) return fail(MOE_ERR_UNSUPPORTED, "this layer's experts have no scales: use moe_load_expert");
+    if (!src_w13_scale || !src_w2_scale || !aligned(src_w13_scale, 4) || !aligned(src_w2_scale, 4))
+        return fail(MOE_ERR_ARG, "src_w13_scale and src_w2_scale must be non-NULL and 4-byte aligned");
+    return fill_slot(l, slot, src_w13, src_w13_scale, src_w2, src_w2_scale, copy_stream, serve_stream, copy_blocks);
 }
 
 moe_status_t moe_workspace_view(const moe_layer_t *l, moe_workspace_view_t *v)
@@ -588,7 +647,7 @@ moe_status_t moe_workspace_view(const moe_layer_t *l, moe_workspace_view_t *v)
     v->offsets = (const int32_t *)(ws + l->lay.offs);
     v->perm = (const int32_t *)(ws + l->lay.perm);
     v->inv = (const int32_t *)(ws + l->lay.inv);
-    v->h = ws + l->lay.h;
+    v->h = ws + (l->scaled() ? l->lay.hq : l->lay.h);
     v->y = ws + l->lay.y;
     v->active_map = (const int32_t *)(ws + l->lay.map);
     v->tiles = (const int32_t *)(ws + l->lay.tiles);
@@ -599,9 +658,66 @@ moe_status_t moe_workspace_view(const moe_layer_t *l, moe_workspace_view_t *v)
     return MOE_OK;
 }
 
+// What is left of a pass of a layer with 8-bit experts: p is filled in but for the tile list's size.
+static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool identity, const void *xq, const float *x_scale, hipStream_t st)
+{
+    char *ws = (char *)l->buf.workspace;
+    const int tile_rows = kStreamMaxRows;
+    const long long assigned = (long long)p.T * p.k + (long long)(p.shared_end - p.shared_begin) * p.n_shared;
+    const long long nonempty = assigned < p.S ? assigned : p.S;
+    const long long tiles_most = (assigned + tile_rows - 1) / tile_rows + nonempty;
+    p.max_tiles = (int)(tiles_most < assigned ? tiles_most : assigned);
+
+    SGemm g1 = {}, g2 = {};
+    g1.a = xq ? (const uint8_t *)xq : (const uint8_t *)(ws + l->lay.xq);
+    g1.as = xq ? x_scale : (const float *)(ws + l->lay.xs);
+    g1.ld_a = p.H; g1.ld_as = scale_blocks(p.H);
+    g1.w = (const uint8_t *)p.w13; g1.ws = l->w13_scale;
+    g1.w_slot = 2 * (size_t)p.I * p.H; g1.ws_slot = 2 * (size_t)scale_blocks(p.I) * scale_blocks(p.H);
+    g1.n = p.I; g1.k = p.H; g1.kb = scale_blocks(p.H);
+    g1.tiles = p.tiles; g1.n_tiles = p.n_tiles; g1.perm = p.perm; g1.max_tiles = p.max_tiles;
+    g1.out = ws + l->lay.h; g1.ld_out = p.I;
+    g2.a = (const uint8_t *)(ws + l->lay.hq); g2.as = (const float *)(ws + l->lay.hs);
+    g2.ld_a = p.I; g2.ld_as = scale_blocks(p.I);
+    g2.w = (const uint8_t *)p.w2; g2.ws = l->w2_scale;
+    g2.w_slot = (size_t)p.H * p.I; g2.ws_slot = (size_t)scale_blocks(p.H) * scale_blocks(p.I);
+    g2.n = p.H; g2.k = p.I; g2.kb = scale_blocks(p.I);
+    g2.tiles = p.tiles; g2.n_tiles = p.n_tiles; g2.max_tiles = p.max_tiles;
+    g2.out = p.y; g2.ld_out = p.H;
+    RowsJob x_rows = {}, h_rows = {};
+    x_rows.rows = p.T; x_rows.cols = p.H; x_rows.x = p.x; x_rows.ld_x = p.H;
+    x_rows.q = (uint8_t *)(ws + l->lay.xq); x_rows.ld_q = p.H; x_rows.scale = (float *)(ws + l->lay.xs); x_rows.ld_scale = g1.ld_as;
+    h_rows.rows = (int32_t)assigned; h_rows.cols = p.I; h_rows.x = g1.out; h_rows.ld_x = p.I;
+    h_rows.q = (uint8_t *)(ws + l->lay.hq); h_rows.ld_q = p.I; h_rows.scale = (float *)(ws + l->lay.hs); h_rows.ld_scale = g2.ld_as;
+
+    hipEvent_t *ev = l->prof_on && l->prof_seen++ % l->prof_every == 0 ? l->ev[l->prof_count % kProfRing] : nullptr;
+    hipError_t e = hipSuccess;
+    const int sel = l->prof_phase;
+    auto mark = [&](int j) { if (ev && e == hipSuccess && (sel < 0 || j == sel || j == sel + 1)) e = hipEventRecord(ev[j], st); };
+    mark(MOE_PHASE_GATE);
+    if (e == hipSuccess && !routed) e = launch_gate(p, st);
+    mark(MOE_PHASE_PERMUTE);
+    if (e == hipSuccess) e = launch_permute(p, tile_rows, false, st);
+    mark(MOE_PHASE_GEMM1);
+    if (e == hipSuccess && identity) e = launch_identity_experts(p, st);
+    if (e == hipSuccess && !identity && !xq) e = launch_rows(x_rows, true, st);
+    if (e == hipSuccess && !identity) e = launch_scaled_stream(g1, true, false, tile_rows, st);
+    if (e == hipSuccess && !identity) e = launch_rows(h_rows, false, st);
+    mark(MOE_PHASE_GEMM2);
+    if (e == hipSuccess && !identity) e = launch_scaled_stream(g2, false, true, tile_rows, st);
+    mark(MOE_PHASE_COMBINE);
+    if (e == hipSuccess) e = launch_combine(p, st);
+    mark(MOE_N_PHASES);
+    if (e != hipSuccess) return fail(MOE_ERR_HIP, "forward launch failed: %s", hipGetErrorString(e));
+    if (ev) l->prof_count++;
+    return MOE_OK;
+}
+
 // One pass; routed_ids/routed_w non-NULL: the gate is skipped and the caller's routing is read in place.
+// xq/x_scale (layers with 8-bit experts): the tokens in 8 bits, or NULL: they are quantised here.
 static moe_status_t forward_pass(moe_layer_t *l, const void *x, int32_t T, const int32_t *routed_ids, const float *routed_w,
-                                 int32_t shared_begin, int32_t shared_end, void *out, void *hip_stream, uint32_t flags)
+                                 int32_t shared_begin, int32_t shared_end, void *out, void *hip_stream, uint32_t flags,
+                                 const void *xq = nullptr, const float *x_scale = nullptr)
 {
     if (!l) return fail(MOE_ERR_ARG, "layer is NULL");
     const moe_config_t &c = l->cfg;
@@ -615,8 +731,10 @@ static moe_status_t forward_pass(moe_layer_t *l, const void *x, int32_t T, const
         const moe_status_t backed = check_owned_backed(l, l->slot_owner, "the active placement names a slot whose page is gone");
         if (backed != MOE_OK) return backed;
     }
+    if (l->scaled() && (flags & MOE_FLAG_FORCE_GENERIC)) return fail(MOE_ERR_UNSUPPORTED, "there are no plain kernels for 8-bit experts");
     if (T == 0) return MOE_OK;
-    if (!x || !out) return fail(MOE_ERR_ARG, "x and out must be non-NULL");
+    const bool needs_x = !(xq && routed_ids) || (flags & MOE_FLAG_IDENTITY_EXPERTS);   // the gate and the identity experts read x itself
+    if ((needs_x && !x) || !out) return fail(MOE_ERR_ARG, "x and out must be non-NULL");
     if (!aligned(x, 16) || !aligned(out, 16)) return fail(MOE_ERR_ARG, "x and out must be 16-byte aligned");
 
     hipStream_t st = (hipStream_t)hip_stream;
@@ -660,6 +778,7 @@ static moe_status_t forward_pass(moe_layer_t *l, const void *x, int32_t T, const
     // gated passes up to kFusedMaxTokens tokens: the selection kernel ranks the assignments, one more kernel places them
     p.fused_hist = !routed_ids && T <= kFusedMaxTokens && T <= p.logit_tokens && !(flags & MOE_FLAG_PERMUTE_UNFUSED);
     const bool identity = flags & MOE_FLAG_IDENTITY_EXPERTS;
+    if (l->scaled()) return scaled_pass(l, p, routed_ids != nullptr, identity, xq, x_scale, st);
     const bool mfma = p.act_bf16 && !(flags & MOE_FLAG_FORCE_GENERIC);
     // bf16 passes: small weight-streaming tasks of one token tile when a slot expects only a handful of rows (tiny; routed: T*k/E on
     // average) and of up to 64 rows for a dozen or two (ring64), the large-tile kernels above that (wide, big), the 128 x 128 kernels for
@@ -822,6 +941,20 @@ moe_status_t moe_forward_routed(moe_layer_t *layer, const void *x, int32_t T, co
     if (T > 0 && (!topk_ids || !topk_w)) return fail(MOE_ERR_ARG, "topk_ids and topk_w must be non-NULL");
     if (!aligned(topk_ids, 4) || !aligned(topk_w, 4)) return fail(MOE_ERR_ARG, "topk_ids and topk_w must be 4-byte aligned");
     return forward_pass(layer, x, T, topk_ids, topk_w, shared_begin, shared_end, out, hip_stream, flags);
+}
+
+moe_status_t moe_forward_scaled(moe_layer_t *layer, const void *x, const void *xq, const float *x_scale, int32_t T, const int32_t *topk_ids, const float *topk_w,
+                                int32_t shared_begin, int32_t shared_end, void *out, void *hip_stream, uint32_t flags)
+{
+    if (!layer) return fail(MOE_ERR_ARG, "layer is NULL");
+    if (!layer->scaled()) return fail(MOE_ERR_UNSUPPORTED, "this layer's experts are not in 8 bits");
+    if (T > 0) {
+        if (!xq || !x_scale) return fail(MOE_ERR_ARG, "xq and x_scale must be non-NULL");
+        if ((topk_ids != nullptr) != (topk_w != nullptr)) return fail(MOE_ERR_ARG, "topk_ids and topk_w must be given together");
+        if (!aligned(xq, 16) || !aligned(x_scale, 4)) return fail(MOE_ERR_ARG, "xq must be 16-byte and x_scale 4-byte aligned");
+        if (!aligned(topk_ids, 4) || !aligned(topk_w, 4)) return fail(MOE_ERR_ARG, "topk_ids and topk_w must be 4-byte aligned");
+    }
+    return forward_pass(layer, x, T, topk_ids, topk_w, shared_begin, shared_end, out, hip_stream, flags, xq, x_scale);
 }
 
 // ---- moe_forward_static: the pass with every intermediate in the library's own device array ----

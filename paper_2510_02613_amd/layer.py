@@ -5,7 +5,7 @@ out, and names the stream.  Nothing in this file computes any step of the layer.
 """
 from __future__ import annotations
 
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -97,18 +97,28 @@ def export_pool(t: torch.Tensor):
     return B.moe_pool_export(t.data_ptr())
 
 
+class ScaledExperts(NamedTuple):
+    """Weight pools of experts held in 8 bits: float8_e4m3fn [S,2I,H] and [S,H,I] with fp32 scales of their 128 x 128 blocks,
+    [S, 2 ceil(I/128), ceil(H/128)] (the gate rows' blocks, then the up rows') and [S, ceil(H/128), ceil(I/128)]."""
+    w13: torch.Tensor
+    w13_scale: torch.Tensor
+    w2: torch.Tensor
+    w2_scale: torch.Tensor
+
+
 class MoELayer:
     """One layer over caller-visible torch buffers.
 
     w13 / w2 are the physical slot pools [S,2I,H] / [S,H,I]; fill or refill slots
-    with `load_slot`, then switch placement with `set_expert_map`.
+    with `load_slot`, then switch placement with `set_expert_map`.  With `scaled` given the experts are held in 8 bits, in
+    those pools (fill them directly, or with `load_expert_async`).
     """
 
     def __init__(self, *, hidden, inter, n_experts, top_k, n_slots, max_tokens, act_dtype="bf16",
                  router_dtype="f32", gate="softmax", n_group=1, topk_group=1, renormalize=True,
                  routed_scale=1.0, n_shared=0, router_w: np.ndarray, logit_bias=None,
                  select_bias=None, device="cuda:0", w13_pool: Optional[VirtualPool] = None,
-                 w2_pool: Optional[VirtualPool] = None):
+                 w2_pool: Optional[VirtualPool] = None, scaled: Optional[ScaledExperts] = None):
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -118,30 +128,42 @@ class MoELayer:
                                else B.MOE_GATE_SIGMOID_GROUP_TOPK, n_group, topk_group,
                                int(renormalize), float(routed_scale), n_shared)
         self.act_dtype = act_dtype
+        self.scaled = scaled
         self.elt = torch.int16 if act_dtype == "bf16" else torch.float32
         self.router_w = _dev(router_w, self.device)
         self.logit_bias = None if logit_bias is None else _dev(np.asarray(logit_bias, np.float32), self.device)
         self.select_bias = None if select_bias is None else _dev(np.asarray(select_bias, np.float32), self.device)
         # the pools: plain allocations, or views of virtual pools the caller maps pages under
-        if w13_pool is None:
+        if scaled is not None:
+            assert w13_pool is None and w2_pool is None, "8-bit pools are given whole"
+            blocks = lambda n: (n + 127) // 128  # noqa: E731
+            for t, dt, shape in ((scaled.w13, torch.float8_e4m3fn, (n_slots, 2 * inter, hidden)), (scaled.w2, torch.float8_e4m3fn, (n_slots, hidden, inter)),
+                                 (scaled.w13_scale, torch.float32, (n_slots, 2 * blocks(inter), blocks(hidden))),
+                                 (scaled.w2_scale, torch.float32, (n_slots, blocks(hidden), blocks(inter)))):
+                assert t.dtype == dt and t.shape == shape and t.is_contiguous() and t.device == self.device, (t.dtype, t.shape, shape)
+            self.w13 = scaled.w13
+        elif w13_pool is None:
             self.w13 = torch.empty((n_slots, 2 * inter, hidden), dtype=self.elt, device=self.device)
         else:
             assert w13_pool.n_vslots == n_slots and w13_pool.slot_shape == (2 * inter, hidden) and w13_pool.elt == self.elt
             self.w13 = w13_pool.tensor
-        if w2_pool is None:
+        if scaled is not None:
+            self.w2 = scaled.w2
+        elif w2_pool is None:
             self.w2 = torch.empty((n_slots, hidden, inter), dtype=self.elt, device=self.device)
         else:
             assert w2_pool.n_vslots == n_slots and w2_pool.slot_shape == (hidden, inter) and w2_pool.elt == self.elt
             self.w2 = w2_pool.tensor
         self.slot13, self.slot2 = self.w13.shape[1:], self.w2.shape[1:]   # one expert's tensors
-        ws_bytes = B.moe_workspace_bytes(self.cfg)
+        ws_bytes = B.moe_workspace_bytes(self.cfg) if scaled is None else B.moe_scaled_workspace_bytes(self.cfg)
         self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
         self.buf = B.MoEBuffers(self.router_w.data_ptr(),
                                 0 if self.logit_bias is None else self.logit_bias.data_ptr(),
                                 0 if self.select_bias is None else self.select_bias.data_ptr(),
                                 self.w13.data_ptr(), self.w2.data_ptr(),
                                 self.workspace.data_ptr(), ws_bytes)
-        self.handle = B.moe_layer_create(self.cfg, self.buf)
+        self.handle = (B.moe_layer_create(self.cfg, self.buf) if scaled is None else
+                       B.moe_layer_create_scaled(self.cfg, self.buf, scaled.w13_scale.data_ptr(), scaled.w2_scale.data_ptr()))
         vp = [p.handle if isinstance(p, VirtualPool) else None for p in (w13_pool, w2_pool)]
         if vp[0] is not None or vp[1] is not None:
             # page pools: the host then refuses placements, fills and forwards that would touch a slot without a page
@@ -161,18 +183,28 @@ class MoELayer:
     # -- weights -------------------------------------------------------------
     def load_slot(self, slot: int, w13: np.ndarray, w2: np.ndarray) -> None:
         """Copy one expert's weights into a physical slot (the stand-in for the paper's
-        p2p-copy of an expert into freshly provided pages)."""
+        p2p-copy of an expert into freshly provided pages).  Not for 8-bit experts, whose pools are the caller's tensors."""
+        assert self.scaled is None
         self.w13[slot].copy_(_dev(w13, self.device))
         self.w2[slot].copy_(_dev(w2, self.device))
 
     def load_pool(self, w13_pool: np.ndarray, w2_pool: np.ndarray) -> None:
+        assert self.scaled is None
         self.w13.copy_(_dev(w13_pool, self.device))
         self.w2.copy_(_dev(w2_pool, self.device))
 
     def load_expert_async(self, slot: int, w13: torch.Tensor, w2: torch.Tensor, copy_stream: torch.cuda.Stream,
-                          serve_stream: Optional[torch.cuda.Stream] = None, copy_blocks: int = 0) -> None:
+                          serve_stream: Optional[torch.cuda.Stream] = None, copy_blocks: int = 0,
+                          w13_scale: Optional[torch.Tensor] = None, w2_scale: Optional[torch.Tensor] = None) -> None:
         """Background fill of a slot that the active map does not use, from device tensors, on copy_stream;
-        the next set_expert_map waits for it."""
+        the next set_expert_map waits for it.  8-bit experts come with their scales."""
+        if self.scaled is not None:
+            for t, pool in ((w13, self.w13), (w2, self.w2), (w13_scale, self.scaled.w13_scale), (w2_scale, self.scaled.w2_scale)):
+                assert t is not None and t.dtype == pool.dtype and t.is_contiguous() and t.shape == pool.shape[1:]
+            B.moe_load_expert_scaled(self.handle, slot, w13.data_ptr(), w13_scale.data_ptr(), w2.data_ptr(), w2_scale.data_ptr(),
+                                     copy_stream.cuda_stream, _stream_ptr(serve_stream, self.device), copy_blocks)
+            return
+        assert w13_scale is None and w2_scale is None
         assert w13.dtype == self.elt and w13.is_contiguous() and w13.shape == self.slot13
         assert w2.dtype == self.elt and w2.is_contiguous() and w2.shape == self.slot2
         s = _stream_ptr(serve_stream, self.device)
@@ -200,12 +232,16 @@ class MoELayer:
                                   None if shared_slots is None or len(shared_slots) == 0 else list(shared_slots), s)
 
     # -- forward -------------------------------------------------------------
+    def _is_act(self, t: torch.Tensor) -> bool:
+        """bf16 rows come as bit patterns (int16); a layer with 8-bit experts takes bfloat16 as well."""
+        return t.dtype == self.elt or (self.scaled is not None and t.dtype == torch.bfloat16)
+
     def upload(self, x: np.ndarray) -> torch.Tensor:
         return _dev(x, self.device)
 
     def forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, shared_range=(0, 0),
                 flags: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        assert x.dtype == self.elt and x.is_contiguous() and x.shape[1] == self.cfg.hidden
+        assert self._is_act(x) and x.is_contiguous() and x.shape[1] == self.cfg.hidden
         T = x.shape[0]
         if out is None:
             out = torch.empty_like(x)
@@ -217,7 +253,10 @@ class MoELayer:
     def forward_static(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, shared_range=(0, 0),
                        flags: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The same pass through moe_forward_static: this layer's configuration, weight buffers and last plain
-        placement, every intermediate in the library's own device array (this layer's workspace is not used)."""
+        placement, every intermediate in the library's own device array (this layer's workspace is not used).  Not for 8-bit
+        experts: that entry takes weights of the activations' type."""
+        if self.scaled is not None:
+            raise ValueError("forward_static does not serve layers with 8-bit experts")
         assert x.dtype == self.elt and x.is_contiguous() and x.shape[1] == self.cfg.hidden
         if out is None:
             out = torch.empty_like(x)
@@ -231,7 +270,7 @@ class MoELayer:
                        out: Optional[torch.Tensor] = None, shared_range=(0, 0), flags: int = 0,
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The pass with the routing given (device int32 ids [T,k], float32 weights [T,k]); no gate."""
-        assert x.dtype == self.elt and x.is_contiguous() and x.shape[1] == self.cfg.hidden
+        assert self._is_act(x) and x.is_contiguous() and x.shape[1] == self.cfg.hidden
         T = x.shape[0]
         assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous() and tuple(topk_ids.shape) == (T, self.cfg.top_k)
         assert topk_w.dtype == torch.float32 and topk_w.is_contiguous() and tuple(topk_w.shape) == (T, self.cfg.top_k)
@@ -241,6 +280,27 @@ class MoELayer:
         s = _stream_ptr(stream, self.device)
         B.moe_forward_routed(self.handle, x.data_ptr(), T, topk_ids.data_ptr(), topk_w.data_ptr(), out.data_ptr(),
                              int(shared_range[0]), int(shared_range[1]), s, flags)
+        return out
+
+    def forward_scaled(self, xq: torch.Tensor, x_scale: torch.Tensor, x: Optional[torch.Tensor] = None, *,
+                       topk_ids: Optional[torch.Tensor] = None, topk_w: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                       shared_range=(0, 0), flags: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """A pass of a layer with 8-bit experts for tokens that are in 8 bits already (scaled.rms_norm writes them).  The routing is
+        given, or the gate runs on x."""
+        T, H, k = xq.shape[0], self.cfg.hidden, self.cfg.top_k
+        assert xq.dtype == torch.float8_e4m3fn and xq.is_contiguous() and xq.shape[1] == H
+        assert x_scale.dtype == torch.float32 and x_scale.is_contiguous() and tuple(x_scale.shape) == (T, (H + 127) // 128) and x_scale.device == xq.device
+        assert x is None or (self._is_act(x) and x.is_contiguous() and tuple(x.shape) == (T, H))
+        assert (topk_ids is None) == (topk_w is None) and (topk_ids is not None or x is not None)
+        if topk_ids is not None:
+            assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous() and tuple(topk_ids.shape) == (T, k) and topk_ids.device == xq.device
+            assert topk_w.dtype == torch.float32 and topk_w.is_contiguous() and tuple(topk_w.shape) == (T, k) and topk_w.device == xq.device
+        if out is None:
+            out = torch.empty((T, H), dtype=torch.bfloat16 if x is None else x.dtype, device=xq.device)
+        assert self._is_act(out) and out.is_contiguous() and tuple(out.shape) == (T, H)
+        B.moe_forward_scaled(self.handle, 0 if x is None else x.data_ptr(), xq.data_ptr(), x_scale.data_ptr(), T,
+                             0 if topk_ids is None else topk_ids.data_ptr(), 0 if topk_w is None else topk_w.data_ptr(), out.data_ptr(),
+                             int(shared_range[0]), int(shared_range[1]), _stream_ptr(stream, self.device), flags)
         return out
 
     # -- intermediates (tests) -------------------------------------------------
@@ -278,6 +338,9 @@ class MoELayer:
             out["units"] = [grab(ptr, 16 * int(min(max(hdr[w, 2], 0), cap)), np.int32, (-1, 4)) for w, ptr in ((0, v.units0), (1, v.units1))]
         es = 2 if self.act_dtype == "bf16" else 4
         npdt = np.uint16 if self.act_dtype == "bf16" else np.float32
-        out["h"] = grab(v.h, es * A * self.cfg.inter, npdt, (A, self.cfg.inter))
+        if self.scaled is None:
+            out["h"] = grab(v.h, es * A * self.cfg.inter, npdt, (A, self.cfg.inter))
+        else:   # e4m3 bit patterns
+            out["h"] = grab(v.h, A * self.cfg.inter, np.uint8, (A, self.cfg.inter))
         out["y"] = grab(v.y, es * A * self.cfg.hidden, npdt, (A, self.cfg.hidden))
         return out
