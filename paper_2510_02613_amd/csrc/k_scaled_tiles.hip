@@ -1,0 +1,397 @@
+// Block-scaled e4m3 products of many rows: tiles of up to 256 rows times 256 weight rows (with swiglu 128 gate and 128 up rows).
+//
+//   out[r, c] = sum_b as[r, b] ws[c / 128, b] sum_{k in block b} a[r, k] w[c, k]
+//
+// A K-step is one scale block: 128 bytes of every row of the tile, one cache line each.  Both operands travel straight from global
+// memory into an LDS ring (16 bytes per lane, the XOR swizzle of swz8 applied on the global side), together with the step's
+// scales, four steps at a time.  The block's sums come out of the matrix cores with a zero start and are added to the
+// fp32 accumulators times as * ws: one multiply-add per four results beside one matrix instruction per 256, which the other
+// wavefront of the SIMD hides.
+//
+// Workgroup: 8 wavefronts as 2 (rows) x 4 (weights).  Wavefront (wm, wn) owns weight rows [64 wn, 64 wn + 64) and the 16-row tiles
+// wm, wm + 2, ... of the rows.  A tile with fewer rows runs a body for fewer of them, whose ring is deeper.
+// Weight rows are the first operand, so that a lane holds four neighbouring columns of one row of the result.  With swiglu
+// 16 gate rows and the 16 matching up rows alternate: a lane has both values of a column in neighbouring accumulators, and the
+// 128 columns of a tile are one scale group of the 8-bit result, whose maximum is found over the four weight wavefronts through LDS.
+#include <type_traits>
+
+#include "scaled.h"
+
+namespace emoe {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kBN = 256;                       // weight rows of a tile
+constexpr int kRowBytes = kScaleBlock;         // bytes of a row in a K-step
+constexpr int kWStage = kBN * kRowBytes;       // 32 KB
+constexpr int kLds = 160 * 1024;
+constexpr int kXcds = 8;
+constexpr int kGroup = 4;                      // steps whose scales travel together
+
+// NT 16-row tiles per wavefront: 32 NT rows
+template <int NT_> struct Ring {
+    static constexpr int NT = NT_, BM = NT * 32, XStage = BM * kRowBytes, Stage = kWStage + XStage;
+    static constexpr int ScaleBytes = 2 * kGroup * BM * 4, WScaleBytes = 2 * 256;
+    static constexpr int NS = (kLds - ScaleBytes - WScaleBytes) / Stage > 4 ? 4 : (kLds - ScaleBytes - WScaleBytes) / Stage;
+    static constexpr int WP = 4, XP = NT >= 2 ? BM / 64 : 1;     // 1 KB pieces (8 rows) per wavefront and step
+    static constexpr int Scales = NS * Stage, WScales = Scales + ScaleBytes;
+    static_assert(NS >= 2 && WScales + WScaleBytes <= kLds, "LDS");
+};
+
+struct Ctx {
+    const uint8_t *wbase, *abase;
+    size_t up;                     // bytes from a gate row to its up row
+    uint32_t woff[4], xoff[4];     // this lane's byte offsets of the pieces it stages, k = 0
+    uint32_t soff;                 // and of its row's scales (wavefronts below BM / 64)
+    const float *sbase, *wsbase;
+    uint32_t wsoff;                // this lane's weight scale of a group: 4 steps of 2 blocks
+    int wave, lane, wm, wn, l15, quad;
+    int k, kb;
+    bool wide;                     // scales of a group travel as 16 bytes
+};
+
+__device__ __forceinline__ uint32_t lds_addr(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
+// global -> LDS: lane i's bytes land at lds + its width * i.  Issued as assembly so that the compiler does not hold later LDS reads for
+// copies of a later stage; wait_loads() waits for them.
+__device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+template <int n>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(n < 64, "vmcnt has 6 bits");
+    __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// The copies of K-step b into its stage.  In a last step that ends inside the block, chunks behind the row's end fetch the step's first one
+// instead (they are zeroed in LDS before use).
+template <typename R, bool kSwiglu>
+__device__ __forceinline__ void issue_step(const Ctx &c, uint32_t stage, int b)
+{
+    const int k0 = b * kRowBytes, left = c.k - k0;
+    const uint8_t *wb = c.wbase + k0, *ab = c.abase + k0;
+#pragma unroll
+    for (int i = 0; i < R::WP; ++i) {
+        const int pc = c.wave * R::WP + i;
+        uint32_t off = c.woff[i];
+        if (left < kRowBytes) {
+            const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
+            if (chunk >= left) off -= chunk;
+        }
+        dma16(kSwiglu && (pc & 2) ? wb + c.up : wb, off, stage + pc * 1024);
+    }
+    if (R::NT >= 2 || c.wave < 4) {
+#pragma unroll
+        for (int i = 0; i < R::XP; ++i) {
+            const int pc = c.wave * R::XP + i;
+            uint32_t off = c.xoff[i];
+            if (left < kRowBytes) {
+                const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
+                if (chunk >= left) off -= chunk;
+            }
+            dma16(ab, off, stage + kWStage + pc * 1024);
+        }
+    }
+}
+// The scales of steps 4 g .. 4 g + 3 into half g & 1 of their buffers (steps that do not exist repeat the last one).
+template <typename R>
+__device__ __forceinline__ void issue_scales(const Ctx &c, uint32_t ring, int g)
+{
+    const int b0 = g * kGroup;
+    if (b0 >= c.kb) return;
+    const uint32_t half = ring + R::Scales + (g & 1) * (R::ScaleBytes / 2);
+    if (c.wave < (R::BM + 63) / 64) {      // 64 rows a wavefront (a tile of 32 rows: the upper lanes repeat the last row, behind its own half)
+        if (c.wide) {
+            if (R::BM >= 64 || c.lane < R::BM) dma16(c.sbase + b0, c.soff, half + c.wave * 1024);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j)
+                if (R::BM >= 64 || c.lane < R::BM) dma4(c.sbase + min(b0 + j, c.kb - 1), c.soff, half + j * R::BM * 4 + c.wave * 256);
+        }
+    }
+    if (c.wave == 7) dma4(c.wsbase + b0, c.wsoff + 4 * min(c.lane & 3, c.kb - 1 - b0), ring + R::WScales + (g & 1) * 256);
+}
+
+// One K-step: NT tiles of 16 rows x 4 tiles of 16 weight rows.  Exact: through bf16, see scaled.h.
+template <int NT, bool kSwiglu, bool kExact>
+__device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, const char *Xs, const float *sa, int sa_row, float sw0, float sw1, f32x4 (&acc)[4][NT])
+{
+    const int lo = ((c.quad ^ swz8(c.l15)) << 4), hi = (((4 + c.quad) ^ swz8(c.l15)) << 4);   // rows 16 apart have the same swizzle but for bit 3 of the row, which l15 holds
+    auto fetch = [&](const char *base, int row16) __attribute__((always_inline)) {
+        const char *p = base + (row16 * 16 + c.l15) * kRowBytes;
+        Bytes32 f;
+        f.lo = *(const uint4 *)(p + lo);
+        f.hi = *(const uint4 *)(p + hi);
+        return f;
+    };
+    typename std::conditional<kExact, Bf16x32, Bytes32>::type wf[4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const Bytes32 f = fetch(Ws, c.wn * 4 + a);
+        if constexpr (kExact) wf[a].from(f); else wf[a] = f;
+    }
+    float s[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[t] = sa[((2 * t + c.wm) * 16 + c.l15) * sa_row];
+    Bytes32 xf[2];
+    xf[0] = fetch(Xs, c.wm);
+    f32x4 d[2][4];
+    auto add = [&](int t) __attribute__((always_inline)) {
+        const float f0 = s[t] * sw0, f1 = kSwiglu ? s[t] * sw1 : f0;
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[a][t][e] = fmaf(d[t & 1][a][e], a & 1 ? f1 : f0, acc[a][t][e]);
+    };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (t + 1 < NT) xf[(t + 1) & 1] = fetch(Xs, 2 * (t + 1) + c.wm);
+        if constexpr (kExact) {
+            Bf16x32 xb;
+            xb.from(xf[t & 1]);
+#pragma unroll
+            for (int a = 0; a < 4; ++a) d[t & 1][a] = multiply_exact(wf[a], xb);
+        } else {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) d[t & 1][a] = multiply_fast(wf[a], xf[t & 1]);
+        }
+        if (t > 0) add(t - 1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    add(NT - 1);
+}
+
+// Rows of the result through a wavefront's own LDS region: 16 rows of 64 fp32 columns, then whole row segments.
+template <int NT, typename TOut>
+__device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const MTile &mt, int n0, char *ring, const f32x4 (&acc)[4][NT])
+{
+    constexpr int STRIDE = 64 + 4;
+    float *mine = (float *)ring + c.wave * 16 * STRIDE;
+    const int col = n0 + c.wn * 64 + (c.lane & 7) * 8, lr = c.lane >> 3;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) *(f32x4 *)(mine + c.l15 * STRIDE + a * 16 + c.quad * 4) = acc[a][t];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += 8) {
+            const int row = (2 * t + c.wm) * 16 + r0 + lr;
+            float v[8];
+            *(f32x4 *)v = *(const f32x4 *)(mine + (r0 + lr) * STRIDE + (c.lane & 7) * 8);
+            *(f32x4 *)(v + 4) = *(const f32x4 *)(mine + (r0 + lr) * STRIDE + (c.lane & 7) * 8 + 4);
+            if (row >= mt.rows || col >= g.n) continue;
+            const size_t r = (size_t)mt.row_begin + row;
+            TOut *o = (TOut *)g.out + r * g.ld_out + col;
+            const TOut *add = g.add ? (const TOut *)g.add + r * g.ld_add + col : nullptr;
+            if (col + 8 <= g.n) {
+                if constexpr (sizeof(TOut) == 4) {
+                    if (add) {
+                        const float4 x = *(const float4 *)add, y = *(const float4 *)(add + 4);
+                        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+                    }
+                    *(float4 *)o = make_float4(v[0], v[1], v[2], v[3]);
+                    *(float4 *)(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+                    if (add) {
+                        const uint4 x = *(const uint4 *)add;
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { v[2 * i] += __uint_as_float(w[i] << 16); v[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
+                    }
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+                    *(uint4 *)o = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else {
+                for (int e = 0; e < g.n - col; ++e) store_f32<TOut>(o, e, v[e] + (add ? load_f32<TOut>(add, e) : 0.f));
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// silu(gate) * up, quantised per row over the tile's 128 columns
+template <int NT>
+__device__ __forceinline__ void store_quantized(const SGemm &g, const Ctx &c, const MTile &mt, int n0, char *ring, f32x4 (&acc)[4][NT])
+{
+    constexpr int BM = NT * 32, STRIDE = 128 + 16;
+    uint32_t *top = (uint32_t *)(ring + BM * STRIDE);          // [BM][4]
+    static_assert(BM * STRIDE + BM * 16 <= kLds, "LDS");
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const bool live = n0 + c.wn * 32 + p * 16 < g.n;      // inter is a multiple of 16
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float h = silu_mul(acc[2 * p][t][e], acc[2 * p + 1][t][e]);
+                acc[2 * p][t][e] = h;
+                m = max(m, live ? magnitude(h) : 0u);
+            }
+        }
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+        if (c.quad == 0) top[((2 * t + c.wm) * 16 + c.l15) * 4 + c.wn] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = (2 * t + c.wm) * 16 + c.l15;
+        const uint4 m = *(const uint4 *)(top + row * 4);
+        const GroupScale s(__uint_as_float(max(max(m.x, m.y), max(m.z, m.w))));
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            *(uint32_t *)(ring + row * STRIDE + c.wn * 32 + p * 16 + c.quad * 4) =
+                pack_e4m3(s.quotient(acc[2 * p][t][0]), s.quotient(acc[2 * p][t][1]), s.quotient(acc[2 * p][t][2]), s.quotient(acc[2 * p][t][3]));
+    }
+    __syncthreads();
+    const int nb = n0 / kScaleBlock;
+    for (int i = threadIdx.x; i < mt.rows * 16; i += kThreads) {
+        const int row = i >> 4, col = n0 + (i & 15) * 8;
+        if (col >= g.n) continue;
+        *(uint2 *)(g.q + ((size_t)mt.row_begin + row) * g.ld_q + col) = *(const uint2 *)(ring + row * STRIDE + (i & 15) * 8);
+    }
+    for (int row = threadIdx.x; row < mt.rows; row += kThreads) {
+        const uint4 m = *(const uint4 *)(top + row * 4);
+        g.qs[((size_t)mt.row_begin + row) * g.ld_qs + nb] = GroupScale::scale(__uint_as_float(max(max(m.x, m.y), max(m.z, m.w))));
+    }
+}
+
+template <int NT, bool kSwiglu, bool kExact, typename TOut>
+__device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt, int n0, char *ring)
+{
+    using R = Ring<NT>;
+    // ---- what this lane copies ----
+#pragma unroll
+    for (int i = 0; i < R::WP; ++i) {
+        const int row = (c.wave * R::WP + i) * 8 + (c.lane >> 3);
+        const int chunk = (c.lane & 7) ^ swz8(row);
+        int col;
+        if (kSwiglu) col = min(n0 + (row >> 5) * 16 + (row & 15), g.n - 1);     // 16 gate rows, 16 up rows, ...
+        else         col = min(n0 + row, g.n - 1);
+        c.woff[i] = (uint32_t)(col - n0) * g.k + chunk * 16;
+    }
+    auto source = [&](int row) { const int r = mt.row_begin + min(row, mt.rows - 1); return g.perm ? g.perm[r] : r; };
+    const int first = g.perm ? 0 : mt.row_begin;           // rows that follow each other are addressed from the tile's first
+    c.abase = g.a + (size_t)first * g.ld_a;
+    c.sbase = g.as + (size_t)first * g.ld_as;
+#pragma unroll
+    for (int i = 0; i < R::XP; ++i) {
+        const int row = (c.wave * R::XP + i) * 8 + (c.lane >> 3);
+        const int chunk = (c.lane & 7) ^ swz8(row);
+        c.xoff[i] = (uint32_t)(source(row) - first) * (uint32_t)g.ld_a + chunk * 16;
+    }
+    c.soff = (uint32_t)(source(c.wave * 64 + c.lane) - first) * (uint32_t)g.ld_as * 4;
+
+    const uint32_t lds = lds_addr(ring);
+    f32x4 acc[4][NT];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[a][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    issue_scales<R>(c, lds, 0);
+#pragma unroll
+    for (int b = 0; b < R::NS - 1; ++b)
+        if (b < c.kb) issue_step<R, kSwiglu>(c, lds + b * R::Stage, b);
+    int stage = 0, fill = R::NS - 1;
+    constexpr int P = R::NT >= 2 ? R::WP + R::XP : R::WP;      // copies of a step that every wavefront issues
+    const int sa_row = c.wide ? kGroup : 1, sa_step = c.wide ? 1 : R::BM;
+    for (int b = 0; b < c.kb; ++b) {
+        // the copies of the younger steps may be on their way (scales among them make the wait stricter, never laxer)
+        if (b + R::NS - 2 < c.kb)                      wait_loads<(R::NS - 2) * P>();
+        else if (R::NS == 4 && b + 1 < c.kb)           wait_loads<P>();
+        else                                           wait_loads<0>();
+        __syncthreads();   // everyone's share of step b is in LDS, and everyone is done with step b - 1
+        char *at = ring + stage * R::Stage;
+        if (c.k - b * kRowBytes < kRowBytes) {
+            // the block's columns behind the end of the rows: zero on both sides
+            const int valid = (c.k - b * kRowBytes) / 16;
+            for (int i = threadIdx.x; i < (kBN + R::BM) * 8; i += kThreads) {
+                const int row = i >> 3;          // weight rows, then rows; both parts start at a multiple of 16 rows
+                if ((i & 7) >= valid) *(uint4 *)(at + row * kRowBytes + (((i & 7) ^ swz8(row < kBN ? row : row - kBN)) << 4)) = make_uint4(0, 0, 0, 0);
+            }
+            __syncthreads();
+        }
+        if ((b & (kGroup - 1)) == 0) issue_scales<R>(c, lds, b / kGroup + 1);
+        if (b + R::NS - 1 < c.kb) {
+            issue_step<R, kSwiglu>(c, lds + fill * R::Stage, b + R::NS - 1);
+            fill = fill + 1 == R::NS ? 0 : fill + 1;
+        }
+        const int half = (b / kGroup) & 1, j = b & (kGroup - 1);
+        const float *sa = (const float *)(ring + R::Scales + half * (R::ScaleBytes / 2)) + j * sa_step;
+        const float *sw = (const float *)(ring + R::WScales + half * 256) + j;
+        const float sw0 = sw[kSwiglu ? 0 : (c.wn >> 1) * 4], sw1 = kSwiglu ? sw[4] : sw0;
+        multiply_step<NT, kSwiglu, kExact>(c, at, at + kWStage, sa, sa_row, sw0, sw1, acc);
+        stage = stage + 1 == R::NS ? 0 : stage + 1;
+    }
+    __syncthreads();   // all reads are done: the ring is the epilogue's
+    if constexpr (kSwiglu) store_quantized<NT>(g, c, mt, n0, ring, acc);
+    else                   store_rows<NT, TOut>(g, c, mt, n0, ring, acc);
+}
+
+// The items of a launch are (tile, slice of the weights); workgroup b works for XCD b % 8, whose share is a run of items.  Tiles are
+// taken `together` at a time, slice by slice, so that a slice's weights are read by that many workgroups of one XCD while they are in its L2.
+template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
+__global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slices, int tile_rows, int together)
+{
+    __shared__ __attribute__((aligned(1024))) char ring[kLds];
+    const int tiles = g.tiles ? *g.n_tiles : (g.m + tile_rows - 1) / tile_rows;
+    const long long items = (long long)tiles * slices, share = (items + kXcds - 1) / kXcds;
+    const long long i = (blockIdx.x % kXcds) * share + blockIdx.x / kXcds;
+    if ((long long)(blockIdx.x / kXcds) >= share || i >= items) return;
+    const int set = (int)(i / ((long long)together * slices)) * together, width = min(together, tiles - set);
+    const int in_set = (int)(i - (long long)set * slices);
+    const int tile = set + in_set % width, n0 = in_set / width * (kSwiglu ? kBN / 2 : kBN);
+    MTile mt = {0, tile * tile_rows, min(tile_rows, g.m - tile * tile_rows), 0};
+    if (g.tiles) mt = g.tiles[tile];
+
+    Ctx c;
+    c.lane = threadIdx.x & 63;
+    c.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    c.wm = c.wave >> 2; c.wn = c.wave & 3;
+    c.l15 = c.lane & 15; c.quad = c.lane >> 4;
+    c.k = g.k; c.kb = g.kb;
+    c.wbase = g.w + (size_t)mt.slot * g.w_slot + (size_t)n0 * g.k;
+    c.up = (size_t)g.n * g.k;
+    const int nb = scale_blocks(g.n), nb0 = n0 / kScaleBlock;
+    c.wsbase = g.ws + (size_t)mt.slot * g.ws_slot + (size_t)nb0 * g.kb;
+    c.wsoff = (c.lane & 4) ? (uint32_t)(kSwiglu ? nb : min(1, nb - 1 - nb0)) * (uint32_t)g.kb * 4 : 0;
+    c.wide = g.kb % kGroup == 0 && g.ld_as % kGroup == 0 && ((uintptr_t)g.as & 15) == 0;
+    const int nt = (mt.rows + 31) >> 5;
+    if (nt <= 1) run_tile<1, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    else if (nt <= 2) run_tile<2, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    else if (kMaxNT <= 4 || nt <= 4) run_tile<4, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    else if constexpr (kMaxNT > 4) {
+        if (nt <= 6) run_tile<6, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+        else         run_tile<8, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    }
+}
+
+template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
+void launch_as(const SGemm &g, int tile_rows, hipStream_t st)
+{
+    const int width = kSwiglu ? kBN / 2 : kBN, slices = (g.n + width - 1) / width;
+    const long long tiles = g.tiles ? g.max_tiles : (g.m + tile_rows - 1) / tile_rows;
+    const long long share = (tiles * slices + kXcds - 1) / kXcds;
+    hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(share * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.tiles ? 2 : 4);
+}
+
+}  // namespace
+
+hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st)
+{
+    if (swiglu) exact ? launch_as<true, true, 4, float>(g, tile_rows, st) : launch_as<true, false, 8, float>(g, tile_rows, st);
+    else        exact ? launch_as<false, true, 4, float>(g, tile_rows, st) : launch_as<false, false, 8, uint16_t>(g, tile_rows, st);
+    return hipGetLastError();
+}
+
+}  // namespace emoe

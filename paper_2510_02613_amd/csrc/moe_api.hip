@@ -93,6 +93,7 @@ moe_status_t check_config(const moe_config_t *c, bool scaled = false)
         if (c->act_dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "8-bit experts take bf16 activations");
         if (c->hidden % 16 || c->inter % 16) return fail(MOE_ERR_UNSUPPORTED, "hidden and inter must be multiples of 16 (16-byte rows of 8-bit values)");
         if (c->hidden > kMaxRowCols || c->inter > kMaxRowCols) return fail(MOE_ERR_UNSUPPORTED, "hidden or inter > %d", kMaxRowCols);
+        if ((long long)c->max_tokens * c->hidden >= (1ll << 32)) return fail(MOE_ERR_UNSUPPORTED, "max_tokens * hidden >= 2^32");
         if ((long long)c->max_tokens * (c->top_k + c->n_shared) > (1ll << 21)) return fail(MOE_ERR_UNSUPPORTED, "max_tokens * (top_k + n_shared) > 2^21");
     }
     return MOE_OK;
@@ -662,7 +663,11 @@ moe_status_t moe_workspace_view(const moe_layer_t *l, moe_workspace_view_t *v)
 static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool identity, const void *xq, const float *x_scale, hipStream_t st)
 {
     char *ws = (char *)l->buf.workspace;
-    const int tile_rows = kStreamMaxRows;
+    const int resident = l->slots_used - p.n_shared < p.E ? l->slots_used - p.n_shared : p.E;
+    const double here = routed ? 1.0 - std::pow(1.0 - (double)resident / p.E, p.k) : 1.0;   // share of all tokens that are sent here
+    const double rows = resident > 0 ? (double)p.T * p.k / p.E / here : 0.0;                // of a slot, for an even load
+    const bool stream = rows <= 16.0;
+    const int tile_rows = stream ? kStreamMaxRows : 256;
     const long long assigned = (long long)p.T * p.k + (long long)(p.shared_end - p.shared_begin) * p.n_shared;
     const long long nonempty = assigned < p.S ? assigned : p.S;
     const long long tiles_most = (assigned + tile_rows - 1) / tile_rows + nonempty;
@@ -677,6 +682,7 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     g1.n = p.I; g1.k = p.H; g1.kb = scale_blocks(p.H);
     g1.tiles = p.tiles; g1.n_tiles = p.n_tiles; g1.perm = p.perm; g1.max_tiles = p.max_tiles;
     g1.out = ws + l->lay.h; g1.ld_out = p.I;
+    g1.q = (uint8_t *)(ws + l->lay.hq); g1.qs = (float *)(ws + l->lay.hs); g1.ld_q = p.I; g1.ld_qs = scale_blocks(p.I);
     g2.a = (const uint8_t *)(ws + l->lay.hq); g2.as = (const float *)(ws + l->lay.hs);
     g2.ld_a = p.I; g2.ld_as = scale_blocks(p.I);
     g2.w = (const uint8_t *)p.w2; g2.ws = l->w2_scale;
@@ -701,10 +707,10 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     mark(MOE_PHASE_GEMM1);
     if (e == hipSuccess && identity) e = launch_identity_experts(p, st);
     if (e == hipSuccess && !identity && !xq) e = launch_rows(x_rows, true, st);
-    if (e == hipSuccess && !identity) e = launch_scaled_stream(g1, true, false, tile_rows, st);
-    if (e == hipSuccess && !identity) e = launch_rows(h_rows, false, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g1, true, false, tile_rows, st) : launch_scaled_tiles(g1, true, false, tile_rows, st);
+    if (e == hipSuccess && !identity && stream) e = launch_rows(h_rows, false, st);
     mark(MOE_PHASE_GEMM2);
-    if (e == hipSuccess && !identity) e = launch_scaled_stream(g2, false, true, tile_rows, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g2, false, true, tile_rows, st) : launch_scaled_tiles(g2, false, false, tile_rows, st);
     mark(MOE_PHASE_COMBINE);
     if (e == hipSuccess) e = launch_combine(p, st);
     mark(MOE_N_PHASES);

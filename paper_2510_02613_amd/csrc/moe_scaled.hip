@@ -23,7 +23,7 @@ moe_status_t fail(moe_status_t st, const char *fmt, ...)
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 constexpr int32_t kMaxRows = 1 << 21;     // rows of a call: grids stay inside the launch limits
-constexpr int64_t kMaxStride = 1 << 23;   // bytes from one 8-bit row to the next: a tile's rows are addressed with 32 bits
+constexpr int64_t kMaxStride = 1 << 23;   // bytes from one 8-bit row to the next, and scales: a tile's rows are addressed with 32 bits
 
 moe_status_t check_dtype(int32_t dtype, const char *what)
 {
@@ -69,8 +69,11 @@ moe_status_t check_product(int32_t m, int32_t n, int32_t k, const void *a, int64
     if (m == 0) return MOE_OK;
     if (!a || !a_scale) return fail(MOE_ERR_ARG, "a and a_scale must be non-NULL");
     if (!aligned(a, 16) || ld_a < k || ld_a % 16) return fail(MOE_ERR_ARG, "a must be 16-byte aligned, its ld (%lld) %d at least and a multiple of 16", (long long)ld_a, k);
+    if (ld_a_scale >= kMaxStride / 4) return fail(MOE_ERR_UNSUPPORTED, "ld of a_scale is %d or larger", (int)(kMaxStride / 4));
     return check_scales(a_scale, ld_a_scale, scale_blocks(k), "a_scale");
 }
+
+bool few_rows(int32_t m) { return m <= kStreamMaxRows; }
 
 SGemm product(int32_t m, int32_t n, int32_t k, const void *a, int64_t ld_a, const float *a_scale, int64_t ld_a_scale, const void *w, const float *w_scale)
 {
@@ -148,14 +151,16 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
     if (p->add) EMOE_TRY(check_rows(p->add, p->ld_add, p->n, p->out_dtype, "add"));
     SGemm g = product(p->m, p->n, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
     g.out = p->out; g.ld_out = p->ld_out; g.add = p->add; g.ld_add = p->ld_add;
-    const hipError_t e = launch_scaled_stream(g, false, p->out_dtype == MOE_BF16, g.m < kStreamMaxRows ? g.m : kStreamMaxRows, (hipStream_t)hip_stream);
+    const bool bf16 = p->out_dtype == MOE_BF16;
+    const hipError_t e = few_rows(g.m) ? launch_scaled_stream(g, false, bf16, g.m, (hipStream_t)hip_stream)
+                                       : launch_scaled_tiles(g, false, !bf16, bf16 ? 256 : 128, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }
 
 size_t moe_scaled_swiglu_workspace_bytes(int32_t m, int32_t inter, int32_t k)
 {
-    if (m <= 0 || inter <= 0 || k <= 0 || m > kMaxRows || inter > kMaxRows) return 0;
+    if (m <= 0 || inter <= 0 || k <= 0 || m > kMaxRows || inter > kMaxRows || !few_rows(m)) return 0;
     return ((size_t)m * inter * 4 + 255) / 256 * 256;
 }
 
@@ -172,9 +177,15 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
     if (need && (!p->workspace || !aligned(p->workspace, 256))) return fail(MOE_ERR_ARG, "workspace must be non-NULL and 256-byte aligned");
     if (p->workspace_bytes < need) return fail(MOE_ERR_CAPACITY, "workspace has %zu bytes, the product needs %zu", p->workspace_bytes, need);
     SGemm g = product(p->m, p->inter, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
-    g.out = p->workspace; g.ld_out = p->inter;
-    hipError_t e = launch_scaled_stream(g, true, false, g.m < kStreamMaxRows ? g.m : kStreamMaxRows, (hipStream_t)hip_stream);
-    if (e == hipSuccess) {
+    hipError_t e = hipSuccess;
+    if (!few_rows(g.m)) {
+        g.q = (uint8_t *)p->q; g.qs = p->q_scale; g.ld_q = p->ld_q; g.ld_qs = p->ld_scale;
+        e = launch_scaled_tiles(g, true, true, 128, (hipStream_t)hip_stream);
+    } else {
+        g.out = p->workspace; g.ld_out = p->inter;
+        e = launch_scaled_stream(g, true, false, g.m, (hipStream_t)hip_stream);
+    }
+    if (e == hipSuccess && few_rows(g.m)) {
         RowsJob j = {};
         j.rows = p->m; j.cols = p->inter;
         j.x = p->workspace; j.ld_x = p->inter;

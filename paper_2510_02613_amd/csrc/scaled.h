@@ -53,6 +53,8 @@ struct SGemm {
 // few rows: the weights are streamed; out fp32 or bf16, swiglu: fp32 rows h
 hipError_t launch_scaled_stream(const SGemm &g, bool swiglu, bool out_bf16, int tile_rows, hipStream_t st);
 constexpr int kStreamMaxRows = 64;
+// many rows: tiles of up to 256 rows (exact: 128); bf16 rows from the 8-bit matrix instructions, fp32 rows from exact products; swiglu: q and qs
+hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st);
 
 #ifdef __HIPCC__
 typedef float f32x4 __attribute__((ext_vector_type(4)));

@@ -90,7 +90,7 @@ def test_quantize_refuses(kw, status):
 
 PRODUCT = [(dict(m=-1), SHAPE), (dict(k=0), SHAPE), (dict(k=264, ld_a=272), UNSUPPORTED), (dict(m=(1 << 21) + 1), UNSUPPORTED), (dict(ld_a=1 << 23), UNSUPPORTED),
            (dict(a=0), ARG), (dict(a=0x10008), ARG), (dict(ld_a=240), ARG), (dict(ld_a=264), ARG), (dict(a_scale=0), ARG), (dict(a_scale=0x20002), ARG),
-           (dict(ld_a_scale=1), ARG), (dict(w=0), ARG), (dict(w=0x30004), ARG), (dict(w_scale=0), ARG), (dict(w_scale=0x40001), ARG)]
+           (dict(ld_a_scale=1), ARG), (dict(ld_a_scale=1 << 21), UNSUPPORTED), (dict(w=0), ARG), (dict(w=0x30004), ARG), (dict(w_scale=0), ARG), (dict(w_scale=0x40001), ARG)]
 
 
 @pytest.mark.parametrize("kw,status", PRODUCT + [
@@ -165,7 +165,7 @@ def layer():
     B.moe_layer_destroy(h)
 
 
-@pytest.mark.parametrize("kw", [dict(act_dtype=B.MOE_F32), dict(hidden=136), dict(inter=72), dict(hidden=32784), dict(inter=40000), dict(max_tokens=(1 << 20) + 1)])
+@pytest.mark.parametrize("kw", [dict(act_dtype=B.MOE_F32), dict(hidden=136), dict(inter=72), dict(hidden=32784), dict(inter=40000), dict(max_tokens=(1 << 20) + 1), dict(hidden=32768, max_tokens=1 << 17)])
 def test_layers_that_cannot_have_8bit_experts(kw):
     cfg = layer_cfg(**kw)
     assert B.lib().moe_scaled_workspace_bytes(ctypes.byref(cfg)) == 0
