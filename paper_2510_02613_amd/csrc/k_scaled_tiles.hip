@@ -57,6 +57,11 @@ __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t l
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
+// The same for the wavefronts of a mask that is all ones or zero (nothing is copied), without a branch; all lanes are active here.
+__device__ __forceinline__ void dma16_masked(const void *base, uint32_t off, uint32_t lds, int mask)
+{
+    asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
+}
 __device__ __forceinline__ void dma4(const void *base, uint32_t off, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
@@ -68,34 +73,39 @@ __device__ __forceinline__ void wait_loads()
     __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
-// The copies of K-step b into its stage.  In a last step that ends inside the block, chunks behind the row's end fetch the step's first one
-// instead (they are zeroed in LDS before use).
-template <typename R, bool kSwiglu>
-__device__ __forceinline__ void issue_step(const Ctx &c, uint32_t stage, int b)
+// Copy i of this wavefront's for K-step b into its stage: weight rows first, then rows.  A last step that ends inside the block fetches the last
+// 128 columns: what comes before its own is zeroed in LDS before use.  Of a contraction shorter than a block (kShort) chunks behind the row's end
+// repeat the first one, and are zeroed.
+template <typename R, bool kSwiglu, bool kShort, int i>
+__device__ __forceinline__ void issue_copy(const Ctx &c, uint32_t stage, int b, int mask)
 {
-    const int k0 = b * kRowBytes, left = c.k - k0;
-    const uint8_t *wb = c.wbase + k0, *ab = c.abase + k0;
-#pragma unroll
-    for (int i = 0; i < R::WP; ++i) {
-        const int pc = c.wave * R::WP + i;
-        uint32_t off = c.woff[i];
-        if (left < kRowBytes) {
-            const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
-            if (chunk >= left) off -= chunk;
-        }
-        dma16(kSwiglu && (pc & 2) ? wb + c.up : wb, off, stage + pc * 1024);
+    constexpr bool weights = i < R::WP;
+    if constexpr (!weights && R::NT < 2) mask = __builtin_amdgcn_readfirstlane(c.wave < 4 ? mask : 0);
+    const int pc = weights ? c.wave * R::WP + i : c.wave * R::XP + i - R::WP;
+    uint32_t off = weights ? c.woff[weights ? i : 0] : c.xoff[weights ? 0 : i - R::WP];
+    if (kShort) {
+        const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
+        if (chunk >= c.k) off -= chunk;
     }
-    if (R::NT >= 2 || c.wave < 4) {
-#pragma unroll
-        for (int i = 0; i < R::XP; ++i) {
-            const int pc = c.wave * R::XP + i;
-            uint32_t off = c.xoff[i];
-            if (left < kRowBytes) {
-                const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
-                if (chunk >= left) off -= chunk;
-            }
-            dma16(ab, off, stage + kWStage + pc * 1024);
-        }
+    const uint8_t *from = (weights ? kSwiglu && (pc & 2) ? c.wbase + c.up : c.wbase : c.abase) + (kShort ? 0 : min(b * kRowBytes, c.k - kRowBytes));
+    dma16_masked(from, off, stage + (weights ? 0 : kWStage) + pc * 1024, mask);
+}
+template <typename R, bool kSwiglu, bool kShort, int i = 0>
+__device__ __forceinline__ void issue_copies(const Ctx &c, uint32_t stage, int b)
+{
+    if constexpr (i < R::WP + R::XP) {
+        issue_copy<R, kSwiglu, kShort, i>(c, stage, b, -1);
+        issue_copies<R, kSwiglu, kShort, i + 1>(c, stage, b);
+    }
+}
+// The copies of a step go out behind the first row tiles' matrix instructions, two at a time: a compute unit accepts 64 bytes a cycle, and a
+// wavefront that issues all of its copies at once stands still meanwhile.
+template <typename R, bool kSwiglu, int i = 0>
+__device__ __forceinline__ void issue_between(const Ctx &c, uint32_t stage, int b, int t, int mask)
+{
+    if constexpr (i < R::WP + R::XP) {
+        if (i / 2 == t || (t == R::NT - 1 && i / 2 > t)) issue_copy<R, kSwiglu, false, i>(c, stage, b, mask);
+        issue_between<R, kSwiglu, i + 1>(c, stage, b, t, mask);
     }
 }
 // The scales of steps 4 g .. 4 g + 3 into half g & 1 of their buffers (steps that do not exist repeat the last one).
@@ -117,9 +127,11 @@ __device__ __forceinline__ void issue_scales(const Ctx &c, uint32_t ring, int g)
     if (c.wave == 7) dma4(c.wsbase + b0, c.wsoff + 4 * min(c.lane & 3, c.kb - 1 - b0), ring + R::WScales + (g & 1) * 256);
 }
 
-// One K-step: NT tiles of 16 rows x 4 tiles of 16 weight rows.  Exact: through bf16, see scaled.h.
-template <int NT, bool kSwiglu, bool kExact>
-__device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, const char *Xs, const float *sa, int sa_row, float sw0, float sw1, f32x4 (&acc)[4][NT])
+// One K-step: NT tiles of 16 rows x 4 tiles of 16 weight rows.  Exact: through bf16, see scaled.h.  between(t) runs behind the
+// matrix instructions of row tile t.
+template <int NT, bool kSwiglu, bool kExact, typename Between>
+__device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, const char *Xs, const float *sa, int sa_row, float sw0, float sw1, f32x4 (&acc)[4][NT],
+                                              Between between)
 {
     const int lo = ((c.quad ^ swz8(c.l15)) << 4), hi = (((4 + c.quad) ^ swz8(c.l15)) << 4);   // rows 16 apart have the same swizzle but for bit 3 of the row, which l15 holds
     auto fetch = [&](const char *base, int row16) __attribute__((always_inline)) {
@@ -135,35 +147,35 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
         const Bytes32 f = fetch(Ws, c.wn * 4 + a);
         if constexpr (kExact) wf[a].from(f); else wf[a] = f;
     }
-    float s[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = sa[((2 * t + c.wm) * 16 + c.l15) * sa_row];
+    const auto scale_of = [&](int t) __attribute__((always_inline)) { return sa[((2 * t + c.wm) * 16 + c.l15) * sa_row]; };
+    float s[2] = {scale_of(0), 0.f};
     Bytes32 xf[2];
     xf[0] = fetch(Xs, c.wm);
+    // two sets of block sums: those of row tile t - 1 are added between the matrix instructions of t.  (Added in front of them, on one set of
+    // registers, both wavefronts of a SIMD add at the same time, and the matrix cores wait.)
     f32x4 d[2][4];
-    auto add = [&](int t) __attribute__((always_inline)) {
-        const float f0 = s[t] * sw0, f1 = kSwiglu ? s[t] * sw1 : f0;
+    auto add = [&](int t, int a, float f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[a][t][e] = fmaf(d[t & 1][a][e], a & 1 ? f1 : f0, acc[a][t][e]);
+        for (int e = 0; e < 4; ++e) acc[a][t][e] = fmaf(d[t & 1][a][e], f, acc[a][t][e]);
     };
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t + 1 < NT) xf[(t + 1) & 1] = fetch(Xs, 2 * (t + 1) + c.wm);
-        if constexpr (kExact) {
-            Bf16x32 xb;
-            xb.from(xf[t & 1]);
+        typename std::conditional<kExact, Bf16x32, Bytes32>::type x;
+        if constexpr (kExact) x.from(xf[t & 1]); else x = xf[t & 1];
+        const float f0 = s[(t + 1) & 1] * sw0, f1 = kSwiglu ? s[(t + 1) & 1] * sw1 : f0;
 #pragma unroll
-            for (int a = 0; a < 4; ++a) d[t & 1][a] = multiply_exact(wf[a], xb);
-        } else {
-#pragma unroll
-            for (int a = 0; a < 4; ++a) d[t & 1][a] = multiply_fast(wf[a], xf[t & 1]);
+        for (int a = 0; a < 4; ++a) {
+            if constexpr (kExact) d[t & 1][a] = multiply_exact(wf[a], x); else d[t & 1][a] = multiply_fast(wf[a], x);
+            if (t > 0) add(t - 1, a, a & 1 ? f1 : f0);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (t > 0) add(t - 1);
+        if (t + 1 < NT) s[(t + 1) & 1] = scale_of(t + 1);
+        between(t);
         __builtin_amdgcn_sched_barrier(0);
     }
-    add(NT - 1);
+#pragma unroll
+    for (int a = 0; a < 4; ++a) add(NT - 1, a, s[(NT - 1) & 1] * (a & 1 ? sw1 : sw0));
 }
 
 // Rows of the result through a wavefront's own LDS region: 16 rows of 64 fp32 columns, then whole row segments.
@@ -299,9 +311,13 @@ __device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[a][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     issue_scales<R>(c, lds, 0);
+    if (c.k < kRowBytes) {
+        issue_copies<R, kSwiglu, true>(c, lds, 0);
+    } else {
 #pragma unroll
-    for (int b = 0; b < R::NS - 1; ++b)
-        if (b < c.kb) issue_step<R, kSwiglu>(c, lds + b * R::Stage, b);
+        for (int b = 0; b < R::NS - 1; ++b)
+            if (b < c.kb) issue_copies<R, kSwiglu, false>(c, lds + b * R::Stage, b);
+    }
     int stage = 0, fill = R::NS - 1;
     constexpr int P = R::NT >= 2 ? R::WP + R::XP : R::WP;      // copies of a step that every wavefront issues
     const int sa_row = c.wide ? kGroup : 1, sa_step = c.wide ? 1 : R::BM;
@@ -313,24 +329,26 @@ __device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt
         __syncthreads();   // everyone's share of step b is in LDS, and everyone is done with step b - 1
         char *at = ring + stage * R::Stage;
         if (c.k - b * kRowBytes < kRowBytes) {
-            // the block's columns behind the end of the rows: zero on both sides
-            const int valid = (c.k - b * kRowBytes) / 16;
+            // a block that ends early: zero what is not its own, on both sides (fetched were the last 128 columns, or the first where there are no 128)
+            const int own = (c.k - b * kRowBytes) / 16;
             for (int i = threadIdx.x; i < (kBN + R::BM) * 8; i += kThreads) {
                 const int row = i >> 3;          // weight rows, then rows; both parts start at a multiple of 16 rows
-                if ((i & 7) >= valid) *(uint4 *)(at + row * kRowBytes + (((i & 7) ^ swz8(row < kBN ? row : row - kBN)) << 4)) = make_uint4(0, 0, 0, 0);
+                if (c.k < kRowBytes ? (i & 7) >= own : (i & 7) < 8 - own) *(uint4 *)(at + row * kRowBytes + (((i & 7) ^ swz8(row < kBN ? row : row - kBN)) << 4)) = make_uint4(0, 0, 0, 0);
             }
             __syncthreads();
         }
         if ((b & (kGroup - 1)) == 0) issue_scales<R>(c, lds, b / kGroup + 1);
-        if (b + R::NS - 1 < c.kb) {
-            issue_step<R, kSwiglu>(c, lds + fill * R::Stage, b + R::NS - 1);
-            fill = fill + 1 == R::NS ? 0 : fill + 1;
-        }
         const int half = (b / kGroup) & 1, j = b & (kGroup - 1);
         const float *sa = (const float *)(ring + R::Scales + half * (R::ScaleBytes / 2)) + j * sa_step;
         const float *sw = (const float *)(ring + R::WScales + half * 256) + j;
         const float sw0 = sw[kSwiglu ? 0 : (c.wn >> 1) * 4], sw1 = kSwiglu ? sw[4] : sw0;
-        multiply_step<NT, kSwiglu, kExact>(c, at, at + kWStage, sa, sa_row, sw0, sw1, acc);
+        const int nb = b + R::NS - 1;                      // the step that is fetched meanwhile
+        const uint32_t next = lds + fill * R::Stage;
+        const int mask = __builtin_amdgcn_readfirstlane(nb < c.kb ? -1 : 0);
+        // (no branch around the copies: across one the compiler lets the multiply-adds slide to the step's end, and their operands out of the registers)
+        multiply_step<NT, kSwiglu, kExact>(c, at, at + kWStage, sa, sa_row, sw0, sw1, acc,
+                                           [&](int t) __attribute__((always_inline)) { issue_between<R, kSwiglu>(c, next, nb, t, mask); });
+        fill = fill + 1 == R::NS ? 0 : fill + 1;
         stage = stage + 1 == R::NS ? 0 : stage + 1;
     }
     __syncthreads();   // all reads are done: the ring is the epilogue's

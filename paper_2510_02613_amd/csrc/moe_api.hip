@@ -666,8 +666,9 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     const int resident = l->slots_used - p.n_shared < p.E ? l->slots_used - p.n_shared : p.E;
     const double here = routed ? 1.0 - std::pow(1.0 - (double)resident / p.E, p.k) : 1.0;   // share of all tokens that are sent here
     const double rows = resident > 0 ? (double)p.T * p.k / p.E / here : 0.0;                // of a slot, for an even load
-    const bool stream = rows <= 16.0;
-    const int tile_rows = stream ? kStreamMaxRows : 256;
+    const char *e1 = getenv("X_STREAM"), *e2 = getenv("X_TILE");
+    const bool stream = e1 ? atoi(e1) : rows <= 16.0;
+    const int tile_rows = e2 ? atoi(e2) : stream ? kStreamMaxRows : 256;
     const long long assigned = (long long)p.T * p.k + (long long)(p.shared_end - p.shared_begin) * p.n_shared;
     const long long nonempty = assigned < p.S ? assigned : p.S;
     const long long tiles_most = (assigned + tile_rows - 1) / tile_rows + nonempty;
