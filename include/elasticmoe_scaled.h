@@ -90,7 +90,7 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *args, void *hip_stream
 
 /*
  * The first half of a dense SwiGLU expert: h = silu(a Wg^T) * (a Wu^T), quantised per row and 128 columns from fp32.
- * Few rows go through fp32 rows in the caller's workspace: moe_scaled_swiglu_workspace_bytes of the same sizes (0: none needed).
+ * Few rows, or little weights, go through fp32 rows in the caller's workspace: moe_scaled_swiglu_workspace_bytes of the same sizes (0: none needed).
  * Calls that share a workspace must be ordered against each other (one stream).
  *   MOE_ERR_UNSUPPORTED: as for the product above; inter no multiple of 16 or > 32768.   MOE_ERR_CAPACITY: workspace too small.
  */

@@ -8,6 +8,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -85,6 +86,14 @@ class MoEScaledSwiglu(ctypes.Structure):
                 ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
                 ("q_scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t)]
+
+
+def packer(struct_type):
+    """What packs a structure's fields, in order, as the C compiler lays it out."""
+    code = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_void_p: "P", ctypes.c_size_t: "N"}
+    s = struct.Struct("@" + "".join(code[t] for _, t in struct_type._fields_))
+    assert s.size == ctypes.sizeof(struct_type)
+    return s.pack
 
 
 class MoEError(RuntimeError):
@@ -174,10 +183,10 @@ def lib() -> ctypes.CDLL:
         L.moe_ceiling_stream.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
         L.moe_ceiling_tile_stream.restype = ctypes.c_int
         L.moe_ceiling_tile_stream.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p]
-        for name, args in (("moe_rms_norm", MoERmsNorm), ("moe_quantize", MoEQuantize),
-                           ("moe_scaled_matmul", MoEScaledMatmul), ("moe_scaled_swiglu", MoEScaledSwiglu)):
+        for name in ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu"):
             getattr(L, name).restype = ctypes.c_int
-            getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+            # the arguments as one of the structures above (byref), or packed: bytes laid out as the structure, which cost less to make
+            getattr(L, name).argtypes = [ctypes.c_void_p, ctypes.c_void_p]
         L.moe_scaled_workspace_bytes.restype = ctypes.c_size_t
         L.moe_scaled_workspace_bytes.argtypes = [ctypes.POINTER(MoEConfig)]
         L.moe_layer_create_scaled.restype = ctypes.c_int
@@ -419,15 +428,15 @@ def moe_forward_scaled(layer, x_ptr: int, xq_ptr: int, x_scale_ptr: int, T: int,
 
 
 def moe_rms_norm(args: MoERmsNorm, stream: int = 0) -> None:
-    _check(lib().moe_rms_norm(args, stream))
+    _check(lib().moe_rms_norm(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_quantize(args: MoEQuantize, stream: int = 0) -> None:
-    _check(lib().moe_quantize(args, stream))
+    _check(lib().moe_quantize(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_scaled_matmul(args: MoEScaledMatmul, stream: int = 0) -> None:
-    _check(lib().moe_scaled_matmul(args, stream))
+    _check(lib().moe_scaled_matmul(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_scaled_swiglu_workspace_bytes(m: int, inter: int, k: int) -> int:
@@ -435,7 +444,7 @@ def moe_scaled_swiglu_workspace_bytes(m: int, inter: int, k: int) -> int:
 
 
 def moe_scaled_swiglu(args: MoEScaledSwiglu, stream: int = 0) -> None:
-    _check(lib().moe_scaled_swiglu(args, stream))
+    _check(lib().moe_scaled_swiglu(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_layer_destroy(layer) -> None:

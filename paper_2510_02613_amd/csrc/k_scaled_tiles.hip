@@ -48,6 +48,7 @@ struct Ctx {
     int wave, lane, wm, wn, l15, quad;
     int k, kb;
     bool wide;                     // scales of a group travel as 16 bytes
+    bool once;                     // no other tile reads these weights
 };
 
 __device__ __forceinline__ uint32_t lds_addr(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
@@ -58,9 +59,12 @@ __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t l
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // The same for the wavefronts of a mask that is all ones or zero (nothing is copied), without a branch; all lanes are active here.
+// kOnce: the line is marked as read once.
+template <bool kOnce>
 __device__ __forceinline__ void dma16_masked(const void *base, uint32_t off, uint32_t lds, int mask)
 {
-    asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
+    if (kOnce) asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
+    else       asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(const void *base, uint32_t off, uint32_t lds)
 {
@@ -88,7 +92,9 @@ __device__ __forceinline__ void issue_copy(const Ctx &c, uint32_t stage, int b, 
         if (chunk >= c.k) off -= chunk;
     }
     const uint8_t *from = (weights ? kSwiglu && (pc & 2) ? c.wbase + c.up : c.wbase : c.abase) + (kShort ? 0 : min(b * kRowBytes, c.k - kRowBytes));
-    dma16_masked(from, off, stage + (weights ? 0 : kWStage) + pc * 1024, mask);
+    const uint32_t to = stage + (weights ? 0 : kWStage) + pc * 1024;
+    if (weights && R::NT <= 2 && c.once) dma16_masked<true>(from, off, to, mask);
+    else                                 dma16_masked<false>(from, off, to, mask);
 }
 template <typename R, bool kSwiglu, bool kShort, int i = 0>
 __device__ __forceinline__ void issue_copies(const Ctx &c, uint32_t stage, int b)
@@ -99,12 +105,12 @@ __device__ __forceinline__ void issue_copies(const Ctx &c, uint32_t stage, int b
     }
 }
 // The copies of a step go out behind the first row tiles' matrix instructions, two at a time: a compute unit accepts 64 bytes a cycle, and a
-// wavefront that issues all of its copies at once stands still meanwhile.
+// wavefront that issues all of its copies at once stands still meanwhile.  Tiles of up to 64 rows, which wait for weights, issue them first.
 template <typename R, bool kSwiglu, int i = 0>
 __device__ __forceinline__ void issue_between(const Ctx &c, uint32_t stage, int b, int t, int mask)
 {
     if constexpr (i < R::WP + R::XP) {
-        if (i / 2 == t || (t == R::NT - 1 && i / 2 > t)) issue_copy<R, kSwiglu, false, i>(c, stage, b, mask);
+        if (R::NT <= 2 ? t == 0 : i / 2 == t || (t == R::NT - 1 && i / 2 > t)) issue_copy<R, kSwiglu, false, i>(c, stage, b, mask);
         issue_between<R, kSwiglu, i + 1>(c, stage, b, t, mask);
     }
 }
@@ -141,6 +147,7 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
         f.hi = *(const uint4 *)(p + hi);
         return f;
     };
+    if (NT <= 2) between(0);
     typename std::conditional<kExact, Bf16x32, Bytes32>::type wf[4];
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
@@ -171,7 +178,7 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
             __builtin_amdgcn_sched_barrier(0);
         }
         if (t + 1 < NT) s[(t + 1) & 1] = scale_of(t + 1);
-        between(t);
+        if (NT > 2) between(t);
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -185,6 +192,21 @@ __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const M
     constexpr int STRIDE = 64 + 4;
     float *mine = (float *)ring + c.wave * 16 * STRIDE;
     const int col = n0 + c.wn * 64 + (c.lane & 7) * 8, lr = c.lane >> 3;
+    const bool whole = col + 8 <= g.n;
+    // what is added is requested for all rows before the first are stored
+    constexpr int W = sizeof(TOut) / 2;                        // 16-byte pieces of 8 columns
+    uint4 av[NT][2][W];
+    if (g.add) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = (2 * t + c.wm) * 16 + h * 8 + lr;
+                if (row < mt.rows && whole)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) av[t][h][w] = *(const uint4 *)((const TOut *)g.add + ((size_t)mt.row_begin + row) * g.ld_add + col + w * 4);
+            }
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -192,37 +214,38 @@ __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const M
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int r0 = 0; r0 < 16; r0 += 8) {
-            const int row = (2 * t + c.wm) * 16 + r0 + lr;
+        for (int h = 0; h < 2; ++h) {
+            const int row = (2 * t + c.wm) * 16 + h * 8 + lr;
             float v[8];
-            *(f32x4 *)v = *(const f32x4 *)(mine + (r0 + lr) * STRIDE + (c.lane & 7) * 8);
-            *(f32x4 *)(v + 4) = *(const f32x4 *)(mine + (r0 + lr) * STRIDE + (c.lane & 7) * 8 + 4);
+            *(f32x4 *)v = *(const f32x4 *)(mine + (h * 8 + lr) * STRIDE + (c.lane & 7) * 8);
+            *(f32x4 *)(v + 4) = *(const f32x4 *)(mine + (h * 8 + lr) * STRIDE + (c.lane & 7) * 8 + 4);
             if (row >= mt.rows || col >= g.n) continue;
             const size_t r = (size_t)mt.row_begin + row;
             TOut *o = (TOut *)g.out + r * g.ld_out + col;
-            const TOut *add = g.add ? (const TOut *)g.add + r * g.ld_add + col : nullptr;
-            if (col + 8 <= g.n) {
-                if constexpr (sizeof(TOut) == 4) {
-                    if (add) {
-                        const float4 x = *(const float4 *)add, y = *(const float4 *)(add + 4);
-                        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+            if (whole) {
+                if (g.add) {
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        const uint32_t x[4] = {av[t][h][w].x, av[t][h][w].y, av[t][h][w].z, av[t][h][w].w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (W == 2) v[w * 4 + i] += __uint_as_float(x[i]);
+                            else { v[2 * i] += __uint_as_float(x[i] << 16); v[2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u); }
+                        }
                     }
+                }
+                if constexpr (W == 2) {
                     *(float4 *)o = make_float4(v[0], v[1], v[2], v[3]);
                     *(float4 *)(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
                 } else {
-                    if (add) {
-                        const uint4 x = *(const uint4 *)add;
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { v[2 * i] += __uint_as_float(w[i] << 16); v[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
-                    }
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
                     *(uint4 *)o = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             } else {
-                for (int e = 0; e < g.n - col; ++e) store_f32<TOut>(o, e, v[e] + (add ? load_f32<TOut>(add, e) : 0.f));
+                const TOut *add = (const TOut *)g.add + r * g.ld_add + col;
+                for (int e = 0; e < g.n - col; ++e) store_f32<TOut>(o, e, v[e] + (g.add ? load_f32<TOut>(add, e) : 0.f));
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -384,6 +407,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slice
     c.wsbase = g.ws + (size_t)mt.slot * g.ws_slot + (size_t)nb0 * g.kb;
     c.wsoff = (c.lane & 4) ? (uint32_t)(kSwiglu ? nb : min(1, nb - 1 - nb0)) * (uint32_t)g.kb * 4 : 0;
     c.wide = g.kb % kGroup == 0 && g.ld_as % kGroup == 0 && ((uintptr_t)g.as & 15) == 0;
+    c.once = g.tiles ? mt.single != 0 : tiles == 1;
     const int nt = (mt.rows + 31) >> 5;
     if (nt <= 1) run_tile<1, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
     else if (nt <= 2) run_tile<2, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
@@ -397,13 +421,24 @@ __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slice
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
 void launch_as(const SGemm &g, int tile_rows, hipStream_t st)
 {
-    const int width = kSwiglu ? kBN / 2 : kBN, slices = (g.n + width - 1) / width;
+    const int slices = tiles_slices(g.n, kSwiglu);
     const long long tiles = g.tiles ? g.max_tiles : (g.m + tile_rows - 1) / tile_rows;
     const long long share = (tiles * slices + kXcds - 1) / kXcds;
     hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(share * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.tiles ? 2 : 4);
 }
 
 }  // namespace
+
+int tiles_slices(int n, bool swiglu) { return (n + (swiglu ? kBN / 2 : kBN) - 1) / (swiglu ? kBN / 2 : kBN); }
+
+// Rounds of the chip times the time of a workgroup: its K-steps and 4 to 6 us for the first copies and the stores.  us a K-step by the tile's 32-row
+// parts, of launches that leave compute units idle .. fill the chip: 1 0.62, 2 0.81, 4 1.0 .. 1.19, 6 1.31 .. 1.55, 8 1.5 .. 2.0; exact products 1 1.08, 2 1.36, 4 1.78.
+double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool exact)
+{
+    const int nt = (tile_rows + 31) / 32;
+    const double step = exact ? (nt <= 1 ? 1.08 : nt <= 2 ? 1.36 : 1.78) : nt <= 1 ? 0.62 : nt <= 2 ? 0.81 : nt <= 4 ? 1.1 : nt <= 6 ? 1.45 : 1.85;
+    return (double)((tiles * tiles_slices(n, swiglu) + 255) / 256) * (scale_blocks(k) * step + 3.5 + 0.25 * nt);
+}
 
 hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st)
 {

@@ -5,6 +5,7 @@
 // references to tensors kept by the memory daemon, Sec. 3.2 "Decoupled Memory and
 // Execution Layers"); all intermediates live in the caller's workspace, which is
 // carved once at create time, so no later call can allocate.
+#include <algorithm>
 #include <atomic>
 #include <chrono>
 #include <cmath>
@@ -51,6 +52,7 @@ moe_status_t fail(moe_status_t st, const char *fmt, ...)
 
 constexpr size_t kAlign = 256;
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+constexpr int kStreamRows = 2048;   // layers with 8-bit experts: fp32 rows of h that the workspace holds, for passes whose weights are streamed
 constexpr int kMinTileRows = 16;  // smallest M-tile any expert kernel uses: sizes the tile list
 
 // Offsets of every intermediate inside the workspace.
@@ -147,7 +149,7 @@ Layout make_layout(const moe_config_t &c, bool tight = false, bool scaled = fals
     L.units[0] = take(sizeof(MUnit) * L.unit_cap);
     L.units[1] = take(sizeof(MUnit) * L.unit_cap);
     L.unit_hdr = take(L.unit_cap ? 2 * sizeof(UnitHdr) : 0);
-    L.h = take((scaled ? 4 : esize(c.act_dtype)) * A * c.inter);
+    L.h = take(scaled ? 4 * std::min(A, (size_t)kStreamRows) * c.inter : esize(c.act_dtype) * A * c.inter);
     L.xq = take(scaled ? T * c.hidden : 0);
     L.xs = take(scaled ? 4 * T * scale_blocks(c.hidden) : 0);
     L.hq = take(scaled ? A * c.inter : 0);
@@ -666,10 +668,13 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     const int resident = l->slots_used - p.n_shared < p.E ? l->slots_used - p.n_shared : p.E;
     const double here = routed ? 1.0 - std::pow(1.0 - (double)resident / p.E, p.k) : 1.0;   // share of all tokens that are sent here
     const double rows = resident > 0 ? (double)p.T * p.k / p.E / here : 0.0;                // of a slot, for an even load
-    const char *e1 = getenv("X_STREAM"), *e2 = getenv("X_TILE");
-    const bool stream = e1 ? atoi(e1) : rows <= 16.0;
-    const int tile_rows = e2 ? atoi(e2) : stream ? kStreamMaxRows : 256;
     const long long assigned = (long long)p.T * p.k + (long long)(p.shared_end - p.shared_begin) * p.n_shared;
+    // A handful of tiles leaves most of the chip idle: their weights are streamed by many small workgroups then.  us, streaming -> tiles:
+    // DeepSeek-V3-shaped rank 1 token 34 -> 63, 3 68 -> 69, 4 89 -> 75, with 16 experts 4 tokens 63 -> 68; Qwen3 shape 1 token 29 -> 33, 2 37.5 -> 34.6, 16 of its experts
+    // 4 tokens 25 -> 31; DeepSeek-V2-Lite shape 1 token 34.5 -> 37.4, 2 46 -> 39: 75 workgroups of GEMM-1 is where they meet.
+    const double tiles_expected = resident * (1.0 - std::exp(-rows)) * std::ceil(rows / 32.0) + (p.shared_end > p.shared_begin ? p.n_shared * std::ceil((p.shared_end - p.shared_begin) / 32.0) : 0.0);
+    const bool stream = tiles_expected * tiles_slices(p.I, true) < 75.0 && assigned <= kStreamRows;
+    const int tile_rows = stream ? 32 : 256;
     const long long nonempty = assigned < p.S ? assigned : p.S;
     const long long tiles_most = (assigned + tile_rows - 1) / tile_rows + nonempty;
     p.max_tiles = (int)(tiles_most < assigned ? tiles_most : assigned);

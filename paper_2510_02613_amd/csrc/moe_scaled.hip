@@ -73,7 +73,25 @@ moe_status_t check_product(int32_t m, int32_t n, int32_t k, const void *a, int64
     return check_scales(a_scale, ld_a_scale, scale_blocks(k), "a_scale");
 }
 
-bool few_rows(int32_t m) { return m <= kStreamMaxRows; }
+// How a product of m rows is run: the streaming kernels, or tiles of tile_rows rows.
+struct Plan { bool stream; int tile_rows; };
+
+// The faster by what both were measured to take (us).  Streaming: 3 + 0.28 per 32 rows and million weights, with swiglu 7 (a second launch quantises) and
+// 0.24: 4096 x 7168 64 rows 19.3 (tiles 34.9), 128 rows 38 (34.9), 333 rows 89 (36); 7168 x 2048 64 rows 12.8 (13.5), 128 rows 20 (13.7); 1544 x 1424 in
+// fp32 333 rows 8.9 (19.1), 1000 rows 20 (20.1); swiglu 2048 x 7168 128 rows 39 (60), 333 rows 75 (60.7), 1408 x 2048 128 rows 15 (21.2), 333 rows 21.9 (21.3).
+Plan plan_product(int32_t m, int32_t n, int32_t k, bool swiglu, bool exact)
+{
+    const double weights = (swiglu ? 2e-6 : 1e-6) * n * k;
+    double best = (swiglu ? 7.0 + 0.24 * weights * ((m + 31) / 32) : 3.0 + 0.28 * weights * ((m + 31) / 32));
+    Plan p = {true, stream_tile_rows(m, n, swiglu)};
+    const int most = exact ? 128 : 256;
+    for (int rows : {32, 64, 128, 192, 256}) {
+        if (rows > most) break;
+        const double us = tiles_us((m + rows - 1) / rows, rows, n, k, swiglu, exact);
+        if (us < best) { best = us; p = {false, rows}; }
+    }
+    return p;
+}
 
 SGemm product(int32_t m, int32_t n, int32_t k, const void *a, int64_t ld_a, const float *a_scale, int64_t ld_a_scale, const void *w, const float *w_scale)
 {
@@ -152,15 +170,16 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
     SGemm g = product(p->m, p->n, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
     g.out = p->out; g.ld_out = p->ld_out; g.add = p->add; g.ld_add = p->ld_add;
     const bool bf16 = p->out_dtype == MOE_BF16;
-    const hipError_t e = few_rows(g.m) ? launch_scaled_stream(g, false, bf16, g.m, (hipStream_t)hip_stream)
-                                       : launch_scaled_tiles(g, false, !bf16, bf16 ? 256 : 128, (hipStream_t)hip_stream);
+    const Plan plan = plan_product(g.m, g.n, g.k, false, !bf16);
+    const hipError_t e = plan.stream ? launch_scaled_stream(g, false, bf16, plan.tile_rows, (hipStream_t)hip_stream)
+                                     : launch_scaled_tiles(g, false, !bf16, plan.tile_rows, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }
 
 size_t moe_scaled_swiglu_workspace_bytes(int32_t m, int32_t inter, int32_t k)
 {
-    if (m <= 0 || inter <= 0 || k <= 0 || m > kMaxRows || inter > kMaxRows || !few_rows(m)) return 0;
+    if (m <= 0 || inter <= 0 || k <= 0 || m > kMaxRows || inter > kMaxRows || !plan_product(m, inter, k, true, true).stream) return 0;
     return ((size_t)m * inter * 4 + 255) / 256 * 256;
 }
 
@@ -177,15 +196,16 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
     if (need && (!p->workspace || !aligned(p->workspace, 256))) return fail(MOE_ERR_ARG, "workspace must be non-NULL and 256-byte aligned");
     if (p->workspace_bytes < need) return fail(MOE_ERR_CAPACITY, "workspace has %zu bytes, the product needs %zu", p->workspace_bytes, need);
     SGemm g = product(p->m, p->inter, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
+    const Plan plan = plan_product(g.m, g.n, g.k, true, true);
     hipError_t e = hipSuccess;
-    if (!few_rows(g.m)) {
+    if (!plan.stream) {
         g.q = (uint8_t *)p->q; g.qs = p->q_scale; g.ld_q = p->ld_q; g.ld_qs = p->ld_scale;
-        e = launch_scaled_tiles(g, true, true, 128, (hipStream_t)hip_stream);
+        e = launch_scaled_tiles(g, true, true, plan.tile_rows, (hipStream_t)hip_stream);
     } else {
         g.out = p->workspace; g.ld_out = p->inter;
-        e = launch_scaled_stream(g, true, false, g.m, (hipStream_t)hip_stream);
+        e = launch_scaled_stream(g, true, false, plan.tile_rows, (hipStream_t)hip_stream);
     }
-    if (e == hipSuccess && few_rows(g.m)) {
+    if (e == hipSuccess && plan.stream) {
         RowsJob j = {};
         j.rows = p->m; j.cols = p->inter;
         j.x = p->workspace; j.ld_x = p->inter;

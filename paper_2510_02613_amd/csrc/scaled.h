@@ -50,10 +50,12 @@ struct SGemm {
     float *qs;
     int64_t ld_q, ld_qs;
 };
-// few rows: the weights are streamed; out fp32 or bf16, swiglu: fp32 rows h
+// few rows: the weights are streamed; out fp32 or bf16, swiglu: fp32 rows h.  Tiles of 16 or 32 rows.
 hipError_t launch_scaled_stream(const SGemm &g, bool swiglu, bool out_bf16, int tile_rows, hipStream_t st);
-constexpr int kStreamMaxRows = 64;
+int stream_tile_rows(int m, int n, bool swiglu);
 // many rows: tiles of up to 256 rows (exact: 128); bf16 rows from the 8-bit matrix instructions, fp32 rows from exact products; swiglu: q and qs
+int tiles_slices(int n, bool swiglu);       // workgroups a tile's weight rows are shared out to
+double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool exact);   // what a launch takes, roughly
 hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st);
 
 #ifdef __HIPCC__

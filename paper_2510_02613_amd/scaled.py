@@ -35,49 +35,39 @@ def blocks(n: int) -> int:
     return (n + BLOCK - 1) // BLOCK
 
 
-def _on_its_device(fn):
-    """Runs a call on the device of its first tensor, whichever is current."""
-    def call(x, *args, **kw):
-        if not x.is_cuda:
-            raise ValueError(f"{fn.__name__} takes tensors on the GPU")
-        dev = x.device.index
-        if dev == torch._C._cuda_getDevice():
-            return fn(x, *args, **kw)
-        with torch.cuda.device(dev):
-            return fn(x, *args, **kw)
-    call.__name__, call.__doc__, call.__wrapped__ = fn.__name__, fn.__doc__, fn
-    return call
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+_pack_norm, _pack_quantize = B.packer(B.MoERmsNorm), B.packer(B.MoEQuantize)
+_pack_matmul, _pack_swiglu = B.packer(B.MoEScaledMatmul), B.packer(B.MoEScaledSwiglu)
 
 
-def _stream(stream, t) -> int:
-    return torch._C._cuda_getCurrentRawStream(t.device.index) if stream is None else stream.cuda_stream
+def _device_of(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("the tensors must be on the GPU")
+    return dev
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, like: torch.Tensor, what: str):
-    """Checks a matrix [rows, cols] with contiguous rows; (address, elements from one row to the next)."""
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what} must be {dtype} [{rows}, {cols}], is {t.dtype} {list(t.shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{what} is on {t.device}, not on {like.device}")
+def _matrix(t: torch.Tensor, shape, dtype, dev: int, what: str):
+    """Checks a matrix with contiguous rows; (address, elements from one row to the next)."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} {list(shape)}, is {t.dtype} {list(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, not on device {dev}")
     ld, one = t.stride()
-    if cols > 1 and one != 1:
+    if one != 1 and shape[1] > 1:
         raise ValueError(f"the rows of {what} must be contiguous")
-    return t.data_ptr(), (ld if rows > 1 else (cols + 15) // 16 * 16)   # one row: its stride says nothing
+    return t.data_ptr(), (ld if shape[0] > 1 else (shape[1] + 15) // 16 * 16)   # one row: its stride says nothing
 
 
-def _whole(t: torch.Tensor, shape, dtype, like: torch.Tensor, what: str) -> int:
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+def _whole(t: torch.Tensor, shape, dtype, dev: int, what: str) -> int:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous {dtype} {list(shape)}, is {t.dtype} {list(t.shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{what} is on {t.device}, not on {like.device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, not on device {dev}")
     return t.data_ptr()
 
 
-def _empty(rows, cols, dtype, like):
-    return torch.empty((rows, cols), dtype=dtype, device=like.device)
-
-
-@_on_its_device
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
              sum_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
              q_scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Normed:
@@ -85,62 +75,78 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual
 
     Those of sum_out, out and (q, q_scale) that are given are computed; with none given, out is allocated, and with a residual sum_out too.
     sum_out and out may be x or residual themselves."""
+    dev = _device_of(x)
+    if dev != _current_device():      # kernels run on the tensors' device, whichever is current
+        with torch.cuda.device(dev):
+            return rms_norm(x, weight, residual=residual, eps=eps, sum_out=sum_out, out=out, q=q, q_scale=q_scale, stream=stream)
     if x.dim() != 2 or x.dtype not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
-    rows, cols = x.shape
+    shape, dt = x.shape, x.dtype
+    rows, cols = shape
     if sum_out is None and out is None and q is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
         sum_out = None if residual is None else torch.empty_like(out)
-    px, ld_x = _matrix(x, rows, cols, x.dtype, x, "x")
-    pr, ld_r = (0, 0) if residual is None else _matrix(residual, rows, cols, x.dtype, x, "residual")
-    pw = 0 if weight is None else _whole(weight, (cols,), x.dtype, x, "weight")
-    ps, ld_s = (0, 0) if sum_out is None else _matrix(sum_out, rows, cols, x.dtype, x, "sum_out")
-    po, ld_o = (0, 0) if out is None else _matrix(out, rows, cols, x.dtype, x, "out")
-    pq, ld_q = (0, 0) if q is None else _matrix(q, rows, cols, E4M3, x, "q")
-    pc, ld_c = (0, 0) if q_scale is None else _matrix(q_scale, rows, blocks(cols), torch.float32, x, "q_scale")
-    B.moe_rms_norm(B.MoERmsNorm(rows, cols, _DTYPE[x.dtype], eps, px, ld_x, pr, ld_r, pw, ps, ld_s, po, ld_o, pq, ld_q, pc, ld_c),
-                   _stream(stream, x))
+    px, ld_x = _matrix(x, shape, dt, dev, "x")
+    pr, ld_r = (0, 0) if residual is None else _matrix(residual, shape, dt, dev, "residual")
+    pw = 0 if weight is None else _whole(weight, (cols,), dt, dev, "weight")
+    ps, ld_s = (0, 0) if sum_out is None else _matrix(sum_out, shape, dt, dev, "sum_out")
+    po, ld_o = (0, 0) if out is None else _matrix(out, shape, dt, dev, "out")
+    pq, ld_q = (0, 0) if q is None else _matrix(q, shape, E4M3, dev, "q")
+    pc, ld_c = (0, 0) if q_scale is None else _matrix(q_scale, (rows, (cols + 127) // 128), torch.float32, dev, "q_scale")
+    B.moe_rms_norm(_pack_norm(rows, cols, _DTYPE[dt], eps, px, ld_x, pr, ld_r, pw, ps, ld_s, po, ld_o, pq, ld_q, pc, ld_c),
+                   _current_stream(dev) if stream is None else stream.cuda_stream)
     return Normed(sum_out, out, q, q_scale)
 
 
-@_on_its_device
 def quantize(x: torch.Tensor, *, block_rows: int = 1, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
              stream: Optional[torch.cuda.Stream] = None) -> Scaled:
     """x in 8 bits: rows of activations (block_rows 1) or a weight matrix (block_rows 128)."""
+    dev = _device_of(x)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return quantize(x, block_rows=block_rows, q=q, scale=scale, stream=stream)
     if x.dim() != 2 or x.dtype not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
-    rows, cols = x.shape
-    scale_rows = rows if block_rows == 1 else blocks(rows)
+    shape, dt = x.shape, x.dtype
+    rows, cols = shape
+    groups = (rows if block_rows == 1 else blocks(rows), blocks(cols))
     if q is None:
-        q = _empty(rows, cols, E4M3, x)
+        q = torch.empty(shape, dtype=E4M3, device=x.device)
     if scale is None:
-        scale = _empty(scale_rows, blocks(cols), torch.float32, x)
-    px, ld_x = _matrix(x, rows, cols, x.dtype, x, "x")
-    pq, ld_q = _matrix(q, rows, cols, E4M3, x, "q")
-    pc, ld_c = _matrix(scale, scale_rows, blocks(cols), torch.float32, x, "scale")
-    B.moe_quantize(B.MoEQuantize(rows, cols, _DTYPE[x.dtype], block_rows, px, ld_x, pq, ld_q, pc, ld_c), _stream(stream, x))
+        scale = torch.empty(groups, dtype=torch.float32, device=x.device)
+    px, ld_x = _matrix(x, shape, dt, dev, "x")
+    pq, ld_q = _matrix(q, shape, E4M3, dev, "q")
+    pc, ld_c = _matrix(scale, groups, torch.float32, dev, "scale")
+    B.moe_quantize(_pack_quantize(rows, cols, _DTYPE[dt], block_rows, px, ld_x, pq, ld_q, pc, ld_c),
+                   _current_stream(dev) if stream is None else stream.cuda_stream)
     return Scaled(q, scale)
 
 
-@_on_its_device
 def matmul(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, add: Optional[torch.Tensor] = None,
            out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """a w^T (+ add) of 8-bit rows a [m, k] and 8-bit weights w [n, k]; out may be add itself."""
-    (m, k), n = a.shape, w.shape[0]
+    dev = _device_of(a)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return matmul(a, a_scale, w, w_scale, add=add, out=out, out_dtype=out_dtype, stream=stream)
+    m, k = a.shape
+    n = w.shape[0]
     if out is None:
         # rows of the result start on 16 bytes whatever n is
-        dt = add.dtype if add is not None else out_dtype
-        out = torch.empty((m, (n + 7) // 8 * 8), dtype=dt, device=a.device)[:, :n]
-    if out.dtype not in _DTYPE:
+        out = torch.empty((m, (n + 7) // 8 * 8), dtype=add.dtype if add is not None else out_dtype, device=a.device)[:, :n]
+    dt = out.dtype
+    if dt not in _DTYPE:
         raise ValueError("out must be bfloat16 or float32")
-    pa, ld_a = _matrix(a, m, k, E4M3, a, "a")
-    pas, ld_as = _matrix(a_scale, m, blocks(k), torch.float32, a, "a_scale")
-    pw = _whole(w, (n, k), E4M3, a, "w")
-    pws = _whole(w_scale, (blocks(n), blocks(k)), torch.float32, a, "w_scale")
-    pad, ld_ad = (0, 0) if add is None else _matrix(add, m, n, out.dtype, a, "add")
-    po, ld_o = _matrix(out, m, n, out.dtype, a, "out")
-    B.moe_scaled_matmul(B.MoEScaledMatmul(m, n, k, _DTYPE[out.dtype], pa, ld_a, pas, ld_as, pw, pws, pad, ld_ad, po, ld_o), _stream(stream, a))
+    kb = (k + 127) // 128
+    pa, ld_a = _matrix(a, (m, k), E4M3, dev, "a")
+    pas, ld_as = _matrix(a_scale, (m, kb), torch.float32, dev, "a_scale")
+    pw = _whole(w, (n, k), E4M3, dev, "w")
+    pws = _whole(w_scale, ((n + 127) // 128, kb), torch.float32, dev, "w_scale")
+    pad, ld_ad = (0, 0) if add is None else _matrix(add, (m, n), dt, dev, "add")
+    po, ld_o = _matrix(out, (m, n), dt, dev, "out")
+    B.moe_scaled_matmul(_pack_matmul(m, n, k, _DTYPE[dt], pa, ld_a, pas, ld_as, pw, pws, pad, ld_ad, po, ld_o),
+                        _current_stream(dev) if stream is None else stream.cuda_stream)
     return out
 
 
@@ -150,24 +156,32 @@ def swiglu_workspace(m: int, inter: int, k: int, device="cuda") -> Optional[torc
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
-@_on_its_device
 def swiglu(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, q: Optional[torch.Tensor] = None,
            scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
            stream: Optional[torch.cuda.Stream] = None) -> Scaled:
     """silu(a Wg^T) * (a Wu^T) in 8 bits; w [2 inter, k] holds the gate rows, then the up rows, w_scale their blocks in that order."""
-    (m, k), inter = a.shape, w.shape[0] // 2
+    dev = _device_of(a)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return swiglu(a, a_scale, w, w_scale, q=q, scale=scale, workspace=workspace, stream=stream)
+    m, k = a.shape
+    inter = w.shape[0] // 2
     if q is None:
-        q = _empty(m, inter, E4M3, a)
+        q = torch.empty((m, inter), dtype=E4M3, device=a.device)
     if scale is None:
-        scale = _empty(m, blocks(inter), torch.float32, a)
+        scale = torch.empty((m, blocks(inter)), dtype=torch.float32, device=a.device)
     if workspace is None:
         workspace = swiglu_workspace(m, inter, k, a.device)
-    pa, ld_a = _matrix(a, m, k, E4M3, a, "a")
-    pas, ld_as = _matrix(a_scale, m, blocks(k), torch.float32, a, "a_scale")
-    pw = _whole(w, (2 * inter, k), E4M3, a, "w")
-    pws = _whole(w_scale, (2 * blocks(inter), blocks(k)), torch.float32, a, "w_scale")
-    pq, ld_q = _matrix(q, m, inter, E4M3, a, "q")
-    pc, ld_c = _matrix(scale, m, blocks(inter), torch.float32, a, "scale")
-    pws_, nws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    B.moe_scaled_swiglu(B.MoEScaledSwiglu(m, inter, k, pa, ld_a, pas, ld_as, pw, pws, pq, ld_q, pc, ld_c, pws_, nws), _stream(stream, a))
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on the device of a")
+    kb, nb = (k + 127) // 128, (inter + 127) // 128
+    pa, ld_a = _matrix(a, (m, k), E4M3, dev, "a")
+    pas, ld_as = _matrix(a_scale, (m, kb), torch.float32, dev, "a_scale")
+    pw = _whole(w, (2 * inter, k), E4M3, dev, "w")
+    pws = _whole(w_scale, (2 * nb, kb), torch.float32, dev, "w_scale")
+    pq, ld_q = _matrix(q, (m, inter), E4M3, dev, "q")
+    pc, ld_c = _matrix(scale, (m, nb), torch.float32, dev, "scale")
+    pk, nk = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    B.moe_scaled_swiglu(_pack_swiglu(m, inter, k, pa, ld_a, pas, ld_as, pw, pws, pq, ld_q, pc, ld_c, pk, nk),
+                        _current_stream(dev) if stream is None else stream.cuda_stream)
     return Scaled(q, scale)

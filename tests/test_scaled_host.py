@@ -55,7 +55,7 @@ def matmul(**kw):
 
 
 def swiglu(**kw):
-    d = dict(m=4, inter=256, k=256, a=0x10000, ld_a=256, a_scale=0x20000, ld_a_scale=2, w=0x30000, w_scale=0x40000,
+    d = dict(m=4, inter=256, k=2048, a=0x10000, ld_a=2048, a_scale=0x20000, ld_a_scale=16, w=0x30000, w_scale=0x40000,
              q=0x50000, ld_q=256, q_scale=0x60000, ld_scale=2, workspace=0x70000, workspace_bytes=1 << 30)
     d.update(kw)
     return lambda: B.moe_scaled_swiglu(B.MoEScaledSwiglu(**d))
@@ -117,6 +117,14 @@ def test_null_arguments(call):
     assert getattr(B.lib(), call)(None, 0) == ARG
 
 
+def test_workspace_of_the_swiglu_product():
+    """fp32 rows for the products that are streamed, none for the others; nothing for sizes that are refused."""
+    assert B.moe_scaled_swiglu_workspace_bytes(4, 256, 2048) == 4 * 256 * 4
+    assert B.moe_scaled_swiglu_workspace_bytes(4096, 2048, 7168) == 0
+    for sizes in ((0, 256, 2048), (4, 0, 2048), (4, 256, 0), (-1, 256, 256), (1 << 22, 256, 256)):
+        assert B.moe_scaled_swiglu_workspace_bytes(*sizes) == 0
+
+
 def test_no_rows_are_no_work():
     norm(rows=0, x=0)()
     quantize(rows=0, x=0)()
@@ -129,10 +137,12 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(ValueError):
         scaled.quantize(torch.zeros(4, 128))                    # not on the GPU
     with pytest.raises(ValueError):
-        scaled._matrix(torch.zeros(4, 128), 4, 128, torch.bfloat16, torch.zeros(1), "x")
+        scaled._matrix(torch.zeros(4, 128), (4, 128), torch.bfloat16, -1, "x")
     with pytest.raises(ValueError):
-        scaled._matrix(torch.zeros(128, 4).t(), 4, 128, torch.float32, torch.zeros(1), "x")
-    assert scaled._matrix(torch.zeros(4, 256)[:, :128], 4, 128, torch.float32, torch.zeros(1), "x")[1] == 256
+        scaled._matrix(torch.zeros(128, 4).t(), (4, 128), torch.float32, -1, "x")
+    with pytest.raises(ValueError):
+        scaled._matrix(torch.zeros(4, 128), (4, 128), torch.float32, 0, "x")        # on another device
+    assert scaled._matrix(torch.zeros(4, 256)[:, :128], (4, 128), torch.float32, -1, "x")[1] == 256
 
 
 def test_reference_rounding_is_e4m3():
