@@ -145,7 +145,9 @@ def test_quantize_extremes(S, block_rows):
 # ---- products ----
 
 MATMUL = [(1, 1, 16), (1, 7168, 2048), (3, 17, 128), (16, 128, 144), (17, 130, 256), (33, 264, 400), (64, 200, 1024), (65, 136, 272),
-          (100, 384, 128), (129, 257, 1168), (257, 520, 640), (300, 1000, 48), (513, 256, 512), (1000, 129, 2048), (40, 768, 7168)]
+          (100, 384, 128), (129, 257, 1168), (257, 520, 640), (300, 1000, 48), (513, 256, 512), (1000, 129, 2048), (40, 768, 7168),
+          # tiles of 32, 64, 128, 192 and 256 rows (fp32 results: up to 128), the last tile one of few rows
+          (2001, 520, 1168), (2000, 1032, 2048), (3000, 1001, 400), (5000, 1100, 272), (4100, 2050, 528), (8201, 1300, 400), (9000, 2100, 112), (8190, 1288, 512)]
 
 
 @pytest.mark.parametrize("m,n,k", MATMUL)
@@ -174,7 +176,7 @@ def test_matmul(S, m, n, k):
 
 
 SWIGLU = [(1, 16, 16), (1, 2048, 512), (2, 128, 128), (17, 1408, 256), (16, 144, 272), (63, 256, 400), (64, 768, 128), (65, 272, 144), (130, 128, 1024),
-          (257, 400, 384), (300, 2048, 128), (600, 136 + 8, 640)]
+          (257, 400, 384), (300, 2048, 128), (600, 136 + 8, 640), (700, 1040, 2064), (2000, 528, 1168), (3001, 400, 400), (2100, 912, 512), (1500, 1040, 96)]
 
 
 @pytest.mark.parametrize("m,inter,k", SWIGLU)
@@ -189,15 +191,35 @@ def test_swiglu(S, m, inter, k):
     assert torch.isnan(rows[m:].float()).all() and torch.isnan(rows[:, inter:].float()).all() and (scales[m:] == 7).all()
 
 
-def test_nan_stays_in_its_row_and_column(S):
-    q, scale, a = eight_bit_rows(5, 70, 384)
-    wq, ws, w = eight_bit_weights(6, 200, 384)
+def test_both_forms_of_the_products_run():
+    """What the sizes above are for: some are streamed, some go through tiles."""
+    from gpu_util import kernels_of
+    from paper_2510_02613_amd import scaled as S
+
+    def names(m, n, k, dtype):
+        q, scale, _ = eight_bit_rows(1, m, k)
+        wq, ws, _ = eight_bit_weights(2, n, k)
+        q, scale, wq, ws, out = q.cuda(), scale.cuda(), wq.cuda(), ws.cuda(), torch.empty(m, n, dtype=dtype, device="cuda")
+        return kernels_of(lambda stream: S.matmul(q, scale, wq, ws, out=out, stream=stream))
+
+    for dtype in (torch.bfloat16, torch.float32):
+        assert ["k_scaled_stream" in n for n in names(16, 128, 144, dtype)] == [True]
+        for m, n, k in ((3000, 1000, 400), (5000, 1104, 272)):
+            assert ["k_scaled_tiles" in n_ for n_ in names(m, n, k, dtype)] == [True]
+
+
+@pytest.mark.parametrize("m", [70, 2100])
+def test_nan_stays_in_its_row_and_column(S, m):
+    q, scale, a = eight_bit_rows(5, m, 384)
+    wq, ws, w = eight_bit_weights(6, 520, 384)
     qn, wn = q.float(), wq.float()
     qn[3, 200] = float("nan")
     wn[150, 7] = float("nan")
     out = S.matmul(qn.to(E4M3).cuda(), scale.cuda(), wn.to(E4M3).cuda(), ws.cuda(), out_dtype=torch.float32).cpu()
-    bad = torch.zeros(70, 200, dtype=torch.bool)
+    bad = torch.zeros(m, 520, dtype=torch.bool)
     bad[3], bad[:, 150] = True, True
+    assert torch.equal(torch.isnan(out), bad)
+    out = S.matmul(qn.to(E4M3).cuda(), scale.cuda(), wn.to(E4M3).cuda(), ws.cuda()).cpu()
     assert torch.equal(torch.isnan(out), bad)
 
 

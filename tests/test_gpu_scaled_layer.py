@@ -121,6 +121,40 @@ def test_routed_pass(shape, T):
     L.close()
 
 
+@pytest.mark.parametrize("H,I", [(256, 272), (400, 256), (512, 384)])
+def test_groups_of_every_size(H, I):
+    """Groups from no row to over a thousand in one pass: tiles of every number of rows, several tiles of a group, and a shared expert."""
+    from gpu_util import kernels_of
+    L = Layer(H=H, I=I, E=12, k=1, n_local=10, n_shared=1, seed=21, max_tokens=2500)
+    counts = [5, 0, 20, 50, 100, 170, 230, 600, 1, 1040]
+    ids = torch.cat([torch.full((n,), e) for e, n in enumerate(counts)] + [torch.full((30,), 11)]).to(torch.int32)
+    ids = ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(1))][:, None].contiguous()
+    T = len(ids)
+    w = torch.rand(T, 1, generator=torch.Generator().manual_seed(2)) + 0.1
+    x, q, scale, value = L.tokens(3, T)
+    q, scale, d_ids, d_w = q.cuda(), scale.cuda(), ids.cuda(), w.cuda()
+    out = torch.empty(T, H, dtype=torch.bfloat16, device="cuda")
+    run = lambda stream=None: L.layer.forward_scaled(q, scale, topk_ids=d_ids, topk_w=d_w, out=out, shared_range=(100, 400), stream=stream)  # noqa: E731
+    assert sum("k_scaled_tiles" in n for n in kernels_of(run)) == 2
+    run()
+    L.check(out, value, ids, w, (100, 400))
+    first = out.clone()
+    run()
+    assert torch.equal(out, first)
+    L.close()
+
+
+def test_few_tokens_are_streamed():
+    from gpu_util import kernels_of
+    L = Layer(**SHAPES[0], seed=0)
+    ids, w = L.routing(7, 3)
+    x, q, scale, _ = L.tokens(9, 3)
+    q, scale, ids, w, out = q.cuda(), scale.cuda(), ids.cuda(), w.cuda(), torch.empty(3, L.H, dtype=torch.bfloat16, device="cuda")
+    names = kernels_of(lambda stream: L.layer.forward_scaled(q, scale, topk_ids=ids, topk_w=w, out=out, stream=stream))
+    assert sum("k_scaled_stream" in n for n in names) == 2
+    L.close()
+
+
 def test_tokens_without_experts_here():
     L = Layer(**SHAPES[1], seed=11)
     T = 20
