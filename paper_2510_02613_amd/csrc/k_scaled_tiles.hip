@@ -185,7 +185,8 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
     for (int a = 0; a < 4; ++a) add(NT - 1, a, s[(NT - 1) & 1] * (a & 1 ? sw1 : sw0));
 }
 
-// Rows of the result through a wavefront's own LDS region: 16 rows of 64 fp32 columns, then whole row segments.
+// Rows of the result through a wavefront's own LDS region: 16 rows of 64 fp32 columns, then whole row segments.  Block16: the wavefront's 64
+// columns of a row become 16-bit numbers with a common scale.
 template <int NT, typename TOut>
 __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const MTile &mt, int n0, char *ring, const f32x4 (&acc)[4][NT])
 {
@@ -194,9 +195,10 @@ __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const M
     const int col = n0 + c.wn * 64 + (c.lane & 7) * 8, lr = c.lane >> 3;
     const bool whole = col + 8 <= g.n;
     // what is added is requested for all rows before the first are stored
+    constexpr bool kBlock = std::is_same<TOut, Block16>::value;
     constexpr int W = sizeof(TOut) / 2;                        // 16-byte pieces of 8 columns
     uint4 av[NT][2][W];
-    if (g.add) {
+    if (!kBlock && g.add) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -219,8 +221,20 @@ __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const M
             float v[8];
             *(f32x4 *)v = *(const f32x4 *)(mine + (h * 8 + lr) * STRIDE + (c.lane & 7) * 8);
             *(f32x4 *)(v + 4) = *(const f32x4 *)(mine + (h * 8 + lr) * STRIDE + (c.lane & 7) * 8 + 4);
-            if (row >= mt.rows || col >= g.n) continue;
             const size_t r = (size_t)mt.row_begin + row;
+            if constexpr (kBlock) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, whole ? magnitude(v[e]) : 0u);
+                top = lanes8_max(top);
+                const Block16Scale b(__uint_as_float(top));
+                if (row < mt.rows && whole) {                  // n is a multiple of 16
+                    *(uint4 *)((uint16_t *)g.out + r * g.ld_out + col) = make_uint4(b.pack(v[0], v[1]), b.pack(v[2], v[3]), b.pack(v[4], v[5]), b.pack(v[6], v[7]));
+                    if ((c.lane & 7) == 0) g.os[r * g.ld_os + (col >> 6)] = b.scale;
+                }
+                continue;
+            }
+            if (row >= mt.rows || col >= g.n) continue;
             TOut *o = (TOut *)g.out + r * g.ld_out + col;
             if (whole) {
                 if (g.add) {
@@ -243,7 +257,7 @@ __device__ __forceinline__ void store_rows(const SGemm &g, const Ctx &c, const M
                     for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
                     *(uint4 *)o = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-            } else {
+            } else if constexpr (!kBlock) {
                 const TOut *add = (const TOut *)g.add + r * g.ld_add + col;
                 for (int e = 0; e < g.n - col; ++e) store_f32<TOut>(o, e, v[e] + (g.add ? load_f32<TOut>(add, e) : 0.f));
             }
@@ -440,10 +454,15 @@ double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool 
     return (double)((tiles * tiles_slices(n, swiglu) + 255) / 256) * (scale_blocks(k) * step + 3.5 + 0.25 * nt);
 }
 
-hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st)
+hipError_t launch_scaled_tiles(const SGemm &g, TilesOut out, int tile_rows, hipStream_t st)
 {
-    if (swiglu) exact ? launch_as<true, true, 4, float>(g, tile_rows, st) : launch_as<true, false, 8, float>(g, tile_rows, st);
-    else        exact ? launch_as<false, true, 4, float>(g, tile_rows, st) : launch_as<false, false, 8, uint16_t>(g, tile_rows, st);
+    switch (out) {
+    case TilesOut::bf16:         launch_as<false, false, 8, uint16_t>(g, tile_rows, st); break;
+    case TilesOut::f32:          launch_as<false, true, 4, float>(g, tile_rows, st); break;
+    case TilesOut::block16:      launch_as<false, false, 8, Block16>(g, tile_rows, st); break;
+    case TilesOut::swiglu:       launch_as<true, false, 8, float>(g, tile_rows, st); break;
+    case TilesOut::swiglu_exact: launch_as<true, true, 4, float>(g, tile_rows, st); break;
+    }
     return hipGetLastError();
 }
 

@@ -58,7 +58,7 @@ constexpr int kMinTileRows = 16;  // smallest M-tile any expert kernel uses: siz
 // Offsets of every intermediate inside the workspace.
 struct Layout {
     size_t map, logits, ids, w, slot_rank, blk_hist, blk_cnt, counts, offs, perm, inv, tiles, n_tiles, units[2], unit_hdr, h, y, partials, total;
-    size_t xq, xs, hq, hs;   // layers with 8-bit experts: the tokens and the rows of h in 8 bits, their scales (h itself: fp32 rows)
+    size_t xq, xs, hq, hs, ys;   // layers with 8-bit experts: the tokens and the rows of h in 8 bits, their scales (h itself: fp32 rows), scales of y
     size_t unit_cap, logit_tokens;
     bool has_partials;
 };
@@ -154,7 +154,8 @@ Layout make_layout(const moe_config_t &c, bool tight = false, bool scaled = fals
     L.xs = take(scaled ? 4 * T * scale_blocks(c.hidden) : 0);
     L.hq = take(scaled ? A * c.inter : 0);
     L.hs = take(scaled ? 4 * A * scale_blocks(c.inter) : 0);
-    L.y = take(esize(c.act_dtype) * A * c.hidden);
+    L.y = take(scaled ? std::max(2 * A, 4 * std::min(A, (size_t)kStreamRows)) * c.hidden : esize(c.act_dtype) * A * c.hidden);
+    L.ys = take(scaled ? 4 * A * scaled_out_groups(c.hidden) : 0);
     // partial sums of split tiles: only layers whose large-tile GEMMs can have contractions long enough to split
     L.has_partials = !scaled && c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (c.hidden >= 4096 || c.inter >= 4096) &&
                      A >= 48 * S;
@@ -695,7 +696,7 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     g2.w_slot = (size_t)p.H * p.I; g2.ws_slot = (size_t)scale_blocks(p.H) * scale_blocks(p.I);
     g2.n = p.H; g2.k = p.I; g2.kb = scale_blocks(p.I);
     g2.tiles = p.tiles; g2.n_tiles = p.n_tiles; g2.max_tiles = p.max_tiles;
-    g2.out = p.y; g2.ld_out = p.H;
+    g2.out = p.y; g2.ld_out = p.H; g2.os = (float *)(ws + l->lay.ys); g2.ld_os = scaled_out_groups(p.H);
     RowsJob x_rows = {}, h_rows = {};
     x_rows.rows = p.T; x_rows.cols = p.H; x_rows.x = p.x; x_rows.ld_x = p.H;
     x_rows.q = (uint8_t *)(ws + l->lay.xq); x_rows.ld_q = p.H; x_rows.scale = (float *)(ws + l->lay.xs); x_rows.ld_scale = g1.ld_as;
@@ -713,12 +714,12 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     mark(MOE_PHASE_GEMM1);
     if (e == hipSuccess && identity) e = launch_identity_experts(p, st);
     if (e == hipSuccess && !identity && !xq) e = launch_rows(x_rows, true, st);
-    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g1, true, false, tile_rows, st) : launch_scaled_tiles(g1, true, false, tile_rows, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g1, true, false, tile_rows, st) : launch_scaled_tiles(g1, TilesOut::swiglu, tile_rows, st);
     if (e == hipSuccess && !identity && stream) e = launch_rows(h_rows, false, st);
     mark(MOE_PHASE_GEMM2);
-    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g2, false, true, tile_rows, st) : launch_scaled_tiles(g2, false, false, tile_rows, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g2, false, false, tile_rows, st) : launch_scaled_tiles(g2, TilesOut::block16, tile_rows, st);
     mark(MOE_PHASE_COMBINE);
-    if (e == hipSuccess) e = launch_combine(p, st);
+    if (e == hipSuccess) e = identity ? launch_combine(p, st) : launch_scaled_combine(p, stream ? nullptr : g2.os, st);
     mark(MOE_N_PHASES);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "forward launch failed: %s", hipGetErrorString(e));
     if (ev) l->prof_count++;

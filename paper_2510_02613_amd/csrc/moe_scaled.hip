@@ -172,7 +172,7 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
     const bool bf16 = p->out_dtype == MOE_BF16;
     const Plan plan = plan_product(g.m, g.n, g.k, false, !bf16);
     const hipError_t e = plan.stream ? launch_scaled_stream(g, false, bf16, plan.tile_rows, (hipStream_t)hip_stream)
-                                     : launch_scaled_tiles(g, false, !bf16, plan.tile_rows, (hipStream_t)hip_stream);
+                                     : launch_scaled_tiles(g, bf16 ? TilesOut::bf16 : TilesOut::f32, plan.tile_rows, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }
@@ -200,7 +200,7 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
     hipError_t e = hipSuccess;
     if (!plan.stream) {
         g.q = (uint8_t *)p->q; g.qs = p->q_scale; g.ld_q = p->ld_q; g.ld_qs = p->ld_scale;
-        e = launch_scaled_tiles(g, true, true, plan.tile_rows, (hipStream_t)hip_stream);
+        e = launch_scaled_tiles(g, TilesOut::swiglu_exact, plan.tile_rows, (hipStream_t)hip_stream);
     } else {
         g.out = p->workspace; g.ld_out = p->inter;
         e = launch_scaled_stream(g, true, false, plan.tile_rows, (hipStream_t)hip_stream);

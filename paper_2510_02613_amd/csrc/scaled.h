@@ -10,6 +10,7 @@ constexpr int kScaleBlock = 128;             // columns (and weight rows) that s
 constexpr float kE4m3Top = 448.f;            // the largest e4m3 value
 constexpr float kZeroGroup = 0x1p-110f;      // a group whose largest magnitude is below this counts as zero (its quotients would leave fp32)
 __host__ __device__ constexpr int scale_blocks(int n) { return (n + kScaleBlock - 1) / kScaleBlock; }
+__host__ __device__ constexpr int scaled_out_groups(int n) { return (n + 63) / 64; }   // of a row of expert outputs
 
 // Rows of values -> their norm, their sum with a residual, their 8-bit form.
 struct RowsJob {
@@ -46,6 +47,8 @@ struct SGemm {
     int64_t ld_out;
     const void *add;              // NULL, or rows of out's type that are added
     int64_t ld_add;
+    float *os;                    // scales of block16 rows
+    int64_t ld_os;
     uint8_t *q;                   // swiglu of the large tiles: 8-bit rows and their scales in the place of out
     float *qs;
     int64_t ld_q, ld_qs;
@@ -53,10 +56,14 @@ struct SGemm {
 // few rows: the weights are streamed; out fp32 or bf16, swiglu: fp32 rows h.  Tiles of 16 or 32 rows.
 hipError_t launch_scaled_stream(const SGemm &g, bool swiglu, bool out_bf16, int tile_rows, hipStream_t st);
 int stream_tile_rows(int m, int n, bool swiglu);
-// many rows: tiles of up to 256 rows (exact: 128); bf16 rows from the 8-bit matrix instructions, fp32 rows from exact products; swiglu: q and qs
+// many rows: tiles of up to 256 rows (exact products: 128).  bf16 rows, the expert outputs of a layer (block16) and its 8-bit rows of h (swiglu) come
+// from the 8-bit matrix instructions, fp32 rows and swiglu_exact's 8-bit ones from exact products.
+enum class TilesOut { bf16, f32, block16, swiglu, swiglu_exact };
 int tiles_slices(int n, bool swiglu);       // workgroups a tile's weight rows are shared out to
 double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool exact);   // what a launch takes, roughly
-hipError_t launch_scaled_tiles(const SGemm &g, bool swiglu, bool exact, int tile_rows, hipStream_t st);
+hipError_t launch_scaled_tiles(const SGemm &g, TilesOut out, int tile_rows, hipStream_t st);
+// the weighted sum of a layer's expert outputs p.y: fp32 rows (scales NULL), or block16 rows with scales [rows][ceil(H/64)]
+hipError_t launch_scaled_combine(const Pass &p, const float *scales, hipStream_t st);
 
 #ifdef __HIPCC__
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -128,6 +135,26 @@ __device__ __forceinline__ uint32_t pack_e4m3(float v0, float v1, float v2, floa
 }
 // magnitudes are compared as integers: a NaN is then larger than all else and makes its whole group NaN, whatever the order
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// Expert outputs between the second GEMM and the weighted sum: 16-bit whole numbers with one fp32 scale, largest magnitude / 32767, for 64 columns of
+// a row.  As many bytes as bf16 and 30 times less rounding (5e-5 of normal values' norm against 1.7e-3): what comes behind, the weighted sum in fp32, is then
+// rounded once, at the end.  A group that holds a NaN or an infinity is NaN throughout.
+struct Block16 { uint16_t v; };
+struct Block16Scale {
+    float scale, r;
+    __device__ __forceinline__ explicit Block16Scale(float top) : scale(top * (1.f / 32767.f)), r(top < kZeroGroup ? 0.f : 32767.f / top) {}
+    __device__ __forceinline__ uint32_t pack(float a, float b) const
+    {
+        return ((uint32_t)__float2int_rn(a * r) & 0xffffu) | ((uint32_t)__float2int_rn(b * r) << 16);
+    }
+};
+// maximum over 8 neighbouring lanes, in all of them
+__device__ __forceinline__ uint32_t lanes8_max(uint32_t v)
+{
+#define EMOE_DPP(ctrl) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false); v = o > v ? o : v; }
+    EMOE_DPP(0xb1) EMOE_DPP(0x4e) EMOE_DPP(0x141)      // lanes 1 and 2 apart, then mirrored in the half row
+#undef EMOE_DPP
+    return v;
+}
 // maximum over the 16 lanes of a DPP row, in all of them
 __device__ __forceinline__ uint32_t row16_max(uint32_t v)
 {

@@ -342,5 +342,6 @@ class MoELayer:
             out["h"] = grab(v.h, es * A * self.cfg.inter, npdt, (A, self.cfg.inter))
         else:   # e4m3 bit patterns
             out["h"] = grab(v.h, A * self.cfg.inter, np.uint8, (A, self.cfg.inter))
-        out["y"] = grab(v.y, es * A * self.cfg.hidden, npdt, (A, self.cfg.hidden))
+        if self.scaled is None:
+            out["y"] = grab(v.y, es * A * self.cfg.hidden, npdt, (A, self.cfg.hidden))
         return out

@@ -92,7 +92,9 @@ class Layer:
             v, dv = R.quantize(h, dh)
             o, do = R.product(v, dv, self.experts[e][5], fast=True)
             y.index_add_(0, token, wt * o)
-            dy.index_add_(0, token, wt * (do + R.BF16 * (o.abs() + do) + 64 * R.F32 * o.abs()))
+            # between the GEMM and the sum: fp32, or 16-bit numbers of a 32767th of the largest of 64 columns, off by half of one
+            top = torch.nn.functional.pad(o.abs() + do, (0, -self.H % 64)).view(len(token), -1, 64).amax(2).repeat_interleave(64, 1)[:, :self.H]
+            dy.index_add_(0, token, wt * (do + top / 65534 * (1 + 2.0 ** -10) + 64 * R.F32 * o.abs()))
         off = (out.cpu().view(torch.bfloat16).double() - y).abs() - dy - (R.BF16 + 64 * R.F32) * (y.abs() + dy)
         assert (off <= 0).all(), f"{off.max().item():.3e} beyond the roundings, of {y.abs().max().item():.3e}"
         return y
