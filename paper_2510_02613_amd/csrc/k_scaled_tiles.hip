@@ -28,9 +28,9 @@ constexpr int kLds = 160 * 1024;
 constexpr int kXcds = 8;
 constexpr int kGroup = 4;                      // steps whose scales travel together
 
-// NT 16-row tiles per wavefront: 32 NT rows
+// NT 16-row tiles per wavefront: 32 NT rows, staged in whole 64
 template <int NT_> struct Ring {
-    static constexpr int NT = NT_, BM = NT * 32, XStage = BM * kRowBytes, Stage = kWStage + XStage;
+    static constexpr int NT = NT_, BM = NT == 1 ? 32 : (NT + 1) / 2 * 64, XStage = BM * kRowBytes, Stage = kWStage + XStage;
     static constexpr int ScaleBytes = 2 * kGroup * BM * 4, WScaleBytes = 2 * 256;
     static constexpr int NS = (kLds - ScaleBytes - WScaleBytes) / Stage > 4 ? 4 : (kLds - ScaleBytes - WScaleBytes) / Stage;
     static constexpr int WP = 4, XP = NT >= 2 ? BM / 64 : 1;     // 1 KB pieces (8 rows) per wavefront and step
@@ -393,8 +393,19 @@ __device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt
     else                   store_rows<NT, TOut>(g, c, mt, n0, ring, acc);
 }
 
+// the body for nt parts of 32 rows
+template <int NT, int kMaxNT, bool kSwiglu, bool kExact, typename TOut>
+__device__ __forceinline__ void run_nt(int nt, const SGemm &g, Ctx &c, const MTile &mt, int n0, char *ring)
+{
+    if constexpr (NT == kMaxNT) run_tile<NT, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    else if (nt <= NT) run_tile<NT, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
+    else run_nt<NT + 1, kMaxNT, kSwiglu, kExact, TOut>(nt, g, c, mt, n0, ring);
+}
+
 // The items of a launch are (tile, slice of the weights); workgroup b works for XCD b % 8, whose share is a run of items.  Tiles are
 // taken `together` at a time, slice by slice, so that a slice's weights are read by that many workgroups of one XCD while they are in its L2.
+// us, 1, 2, 4 at a time: 8192^3 493, 466, 456; layers, where as many belong together as a slot has tiles: DeepSeek-V3-shaped rank 8192 routed tokens, two
+// tiles a slot, 860, 841, 846, 3000 tokens, one, 467, 497, 516; Qwen3 shape 4096 tokens, one or two, 323, 332, 352.
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
 __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slices, int tile_rows, int together)
 {
@@ -423,13 +434,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slice
     c.wide = g.kb % kGroup == 0 && g.ld_as % kGroup == 0 && ((uintptr_t)g.as & 15) == 0;
     c.once = g.tiles ? mt.single != 0 : tiles == 1;
     const int nt = (mt.rows + 31) >> 5;
-    if (nt <= 1) run_tile<1, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
-    else if (nt <= 2) run_tile<2, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
-    else if (kMaxNT <= 4 || nt <= 4) run_tile<4, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
-    else if constexpr (kMaxNT > 4) {
-        if (nt <= 6) run_tile<6, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
-        else         run_tile<8, kSwiglu, kExact, TOut>(g, c, mt, n0, ring);
-    }
+    run_nt<1, kMaxNT, kSwiglu, kExact, TOut>(nt, g, c, mt, n0, ring);
 }
 
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
@@ -438,7 +443,7 @@ void launch_as(const SGemm &g, int tile_rows, hipStream_t st)
     const int slices = tiles_slices(g.n, kSwiglu);
     const long long tiles = g.tiles ? g.max_tiles : (g.m + tile_rows - 1) / tile_rows;
     const long long share = (tiles * slices + kXcds - 1) / kXcds;
-    hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(share * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.tiles ? 2 : 4);
+    hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(share * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.together);
 }
 
 }  // namespace

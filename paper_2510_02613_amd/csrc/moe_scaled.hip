@@ -99,6 +99,7 @@ SGemm product(int32_t m, int32_t n, int32_t k, const void *a, int64_t ld_a, cons
     g.a = (const uint8_t *)a; g.as = a_scale; g.ld_a = ld_a; g.ld_as = ld_a_scale;
     g.w = (const uint8_t *)w; g.ws = w_scale;
     g.m = m; g.n = n; g.k = k; g.kb = scale_blocks(k);
+    g.together = 4;
     return g;
 }
 

@@ -42,6 +42,7 @@ struct SGemm {
     const int32_t *n_tiles;
     const int32_t *perm;
     int32_t max_tiles;
+    int32_t together;             // tiles that share weights and are worked on side by side
     // result rows; with swiglu silu(gate) * up
     void *out;
     int64_t ld_out;
