@@ -28,14 +28,20 @@ constexpr int kLds = 160 * 1024;
 constexpr int kXcds = 8;
 constexpr int kGroup = 4;                      // steps whose scales travel together
 
-// NT 16-row tiles per wavefront: 32 NT rows, staged in whole 64
+// NT 16-row tiles per wavefront: 32 NT rows, staged in whole 64.  NW stages of weights, NX of rows: as many as there is room for, weights first,
+// which come from memory while the rows are found in L2.
 template <int NT_> struct Ring {
-    static constexpr int NT = NT_, BM = NT == 1 ? 32 : (NT + 1) / 2 * 64, XStage = BM * kRowBytes, Stage = kWStage + XStage;
-    static constexpr int ScaleBytes = 2 * kGroup * BM * 4, WScaleBytes = 2 * 256;
-    static constexpr int NS = (kLds - ScaleBytes - WScaleBytes) / Stage > 4 ? 4 : (kLds - ScaleBytes - WScaleBytes) / Stage;
+    static constexpr int NT = NT_, BM = NT == 1 ? 32 : (NT + 1) / 2 * 64, XStage = BM * kRowBytes;
+    static constexpr int NW = NT <= 2 ? 4 : NT <= 6 ? 3 : 2, NX = NT == 1 ? 4 : NT <= 4 ? 3 : 2;
     static constexpr int WP = 4, XP = NT >= 2 ? BM / 64 : 1;     // 1 KB pieces (8 rows) per wavefront and step
-    static constexpr int Scales = NS * Stage, WScales = Scales + ScaleBytes;
-    static_assert(NS >= 2 && WScales + WScaleBytes <= kLds, "LDS");
+    static constexpr int XBase = NW * kWStage, Scales = XBase + NX * XStage, ScaleBytes = 2 * kGroup * BM * 4;
+    static constexpr int WScales = Scales + ScaleBytes, WScaleBytes = 2 * 256;
+    // Copies that may be on their way when step b is needed, all steps up to b + NW - 2 being there: in the order in which they go out (the rows of a step
+    // before its weights) those behind the rows of b, or with as many stages of both behind its weights.  A wavefront that issues more waits for more.
+    static constexpr int P = NT >= 2 ? WP + XP : WP;
+    static constexpr int Young = (NX - 2) * P + (NW > NX ? WP : 0);
+    static_assert(NW == NX || NW == NX + 1, "Young");
+    static_assert(WScales + WScaleBytes <= kLds, "LDS");
 };
 
 struct Ctx {
@@ -63,6 +69,7 @@ __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t l
 template <bool kOnce>
 __device__ __forceinline__ void dma16_masked(const void *base, uint32_t off, uint32_t lds, int mask)
 {
+    mask = __builtin_amdgcn_readfirstlane(mask);
     if (kOnce) asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
     else       asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(lds), "v"(off), "s"(base), "s"(mask) : "memory", "m0");
 }
@@ -77,41 +84,43 @@ __device__ __forceinline__ void wait_loads()
     __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
-// Copy i of this wavefront's for K-step b into its stage: weight rows first, then rows.  A last step that ends inside the block fetches the last
-// 128 columns: what comes before its own is zeroed in LDS before use.  Of a contraction shorter than a block (kShort) chunks behind the row's end
-// repeat the first one, and are zeroed.
+// Copy i of this wavefront's for a K-step: rows of step b + NX - 1 first, then weights of step b + NW - 1 (step b is the one that is multiplied meanwhile).
+// A last step that ends inside the block fetches the last 128 columns: what comes before its own is zeroed in LDS before use.  Of a contraction shorter
+// than a block (kShort) chunks behind the row's end repeat the first one, and are zeroed.
 template <typename R, bool kSwiglu, bool kShort, int i>
-__device__ __forceinline__ void issue_copy(const Ctx &c, uint32_t stage, int b, int mask)
+__device__ __forceinline__ void issue_copy(const Ctx &c, uint32_t lds, int wstage, int xstage, int b)
 {
-    constexpr bool weights = i < R::WP;
-    if constexpr (!weights && R::NT < 2) mask = __builtin_amdgcn_readfirstlane(c.wave < 4 ? mask : 0);
-    const int pc = weights ? c.wave * R::WP + i : c.wave * R::XP + i - R::WP;
-    uint32_t off = weights ? c.woff[weights ? i : 0] : c.xoff[weights ? 0 : i - R::WP];
+    constexpr bool weights = i >= R::XP;
+    const int step = b + (weights ? R::NW : R::NX) - 1;
+    int mask = step >= 0 && step < c.kb ? -1 : 0;
+    if constexpr (!weights && R::NT < 2) mask = c.wave < 4 ? mask : 0;
+    const int pc = weights ? c.wave * R::WP + i - R::XP : c.wave * R::XP + i;
+    uint32_t off = weights ? c.woff[weights ? i - R::XP : 0] : c.xoff[weights ? 0 : i];
     if (kShort) {
         const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
         if (chunk >= c.k) off -= chunk;
     }
-    const uint8_t *from = (weights ? kSwiglu && (pc & 2) ? c.wbase + c.up : c.wbase : c.abase) + (kShort ? 0 : min(b * kRowBytes, c.k - kRowBytes));
-    const uint32_t to = stage + (weights ? 0 : kWStage) + pc * 1024;
+    const uint8_t *from = (weights ? kSwiglu && (pc & 2) ? c.wbase + c.up : c.wbase : c.abase) + (kShort ? 0 : min(step * kRowBytes, c.k - kRowBytes));
+    const uint32_t to = lds + (weights ? wstage * kWStage : R::XBase + xstage * R::XStage) + pc * 1024;
     if (weights && R::NT <= 2 && c.once) dma16_masked<true>(from, off, to, mask);
     else                                 dma16_masked<false>(from, off, to, mask);
 }
 template <typename R, bool kSwiglu, bool kShort, int i = 0>
-__device__ __forceinline__ void issue_copies(const Ctx &c, uint32_t stage, int b)
+__device__ __forceinline__ void issue_copies(const Ctx &c, uint32_t lds, int wstage, int xstage, int b)
 {
     if constexpr (i < R::WP + R::XP) {
-        issue_copy<R, kSwiglu, kShort, i>(c, stage, b, -1);
-        issue_copies<R, kSwiglu, kShort, i + 1>(c, stage, b);
+        issue_copy<R, kSwiglu, kShort, i>(c, lds, wstage, xstage, b);
+        issue_copies<R, kSwiglu, kShort, i + 1>(c, lds, wstage, xstage, b);
     }
 }
 // The copies of a step go out behind the first row tiles' matrix instructions, two at a time: a compute unit accepts 64 bytes a cycle, and a
 // wavefront that issues all of its copies at once stands still meanwhile.  Tiles of up to 64 rows, which wait for weights, issue them first.
 template <typename R, bool kSwiglu, int i = 0>
-__device__ __forceinline__ void issue_between(const Ctx &c, uint32_t stage, int b, int t, int mask)
+__device__ __forceinline__ void issue_between(const Ctx &c, uint32_t lds, int wstage, int xstage, int b, int t)
 {
     if constexpr (i < R::WP + R::XP) {
-        if (R::NT <= 2 ? t == 0 : i / 2 == t || (t == R::NT - 1 && i / 2 > t)) issue_copy<R, kSwiglu, false, i>(c, stage, b, mask);
-        issue_between<R, kSwiglu, i + 1>(c, stage, b, t, mask);
+        if (R::NT <= 2 ? t == 0 : i / 2 == t || (t == R::NT - 1 && i / 2 > t)) issue_copy<R, kSwiglu, false, i>(c, lds, wstage, xstage, b);
+        issue_between<R, kSwiglu, i + 1>(c, lds, wstage, xstage, b, t);
     }
 }
 // The scales of steps 4 g .. 4 g + 3 into half g & 1 of their buffers (steps that do not exist repeat the last one).
@@ -348,29 +357,28 @@ __device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[a][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     issue_scales<R>(c, lds, 0);
+    // as the steps before the first would have done: step -1 fills the last stage but one of the weights and of the rows
     if (c.k < kRowBytes) {
-        issue_copies<R, kSwiglu, true>(c, lds, 0);
+        issue_copies<R, kSwiglu, true>(c, lds, 0, 0, 1 - R::NW);              // the weights of step 0, and with as many stages its rows
+        if (R::NX != R::NW) issue_copies<R, kSwiglu, true>(c, lds, 1, 0, 1 - R::NX);
     } else {
 #pragma unroll
-        for (int b = 0; b < R::NS - 1; ++b)
-            if (b < c.kb) issue_copies<R, kSwiglu, false>(c, lds + b * R::Stage, b);
+        for (int b = 1 - R::NW; b < 0; ++b) issue_copies<R, kSwiglu, false>(c, lds, b + R::NW - 1, max(0, b + R::NX - 1), b);
     }
-    int stage = 0, fill = R::NS - 1;
-    constexpr int P = R::NT >= 2 ? R::WP + R::XP : R::WP;      // copies of a step that every wavefront issues
+    int wat = 0, xat = 0, wfill = R::NW - 1, xfill = R::NX - 1;     // stages of step b, and of those that are fetched meanwhile
     const int sa_row = c.wide ? kGroup : 1, sa_step = c.wide ? 1 : R::BM;
     for (int b = 0; b < c.kb; ++b) {
-        // the copies of the younger steps may be on their way (scales among them make the wait stricter, never laxer)
-        if (b + R::NS - 2 < c.kb)                      wait_loads<(R::NS - 2) * P>();
-        else if (R::NS == 4 && b + 1 < c.kb)           wait_loads<P>();
-        else                                           wait_loads<0>();
+        if (b + R::NW - 2 < c.kb) wait_loads<R::Young>();
+        else                      wait_loads<0>();
         __syncthreads();   // everyone's share of step b is in LDS, and everyone is done with step b - 1
-        char *at = ring + stage * R::Stage;
+        char *ws = ring + wat * kWStage, *xs = ring + R::XBase + xat * R::XStage;
         if (c.k - b * kRowBytes < kRowBytes) {
             // a block that ends early: zero what is not its own, on both sides (fetched were the last 128 columns, or the first where there are no 128)
             const int own = (c.k - b * kRowBytes) / 16;
             for (int i = threadIdx.x; i < (kBN + R::BM) * 8; i += kThreads) {
-                const int row = i >> 3;          // weight rows, then rows; both parts start at a multiple of 16 rows
-                if (c.k < kRowBytes ? (i & 7) >= own : (i & 7) < 8 - own) *(uint4 *)(at + row * kRowBytes + (((i & 7) ^ swz8(row < kBN ? row : row - kBN)) << 4)) = make_uint4(0, 0, 0, 0);
+                const int r = i >> 3, row = r < kBN ? r : r - kBN;
+                if (c.k < kRowBytes ? (i & 7) >= own : (i & 7) < 8 - own)
+                    *(uint4 *)((r < kBN ? ws : xs) + row * kRowBytes + (((i & 7) ^ swz8(row)) << 4)) = make_uint4(0, 0, 0, 0);
             }
             __syncthreads();
         }
@@ -379,14 +387,13 @@ __device__ __forceinline__ void run_tile(const SGemm &g, Ctx &c, const MTile &mt
         const float *sa = (const float *)(ring + R::Scales + half * (R::ScaleBytes / 2)) + j * sa_step;
         const float *sw = (const float *)(ring + R::WScales + half * 256) + j;
         const float sw0 = sw[kSwiglu ? 0 : (c.wn >> 1) * 4], sw1 = kSwiglu ? sw[4] : sw0;
-        const int nb = b + R::NS - 1;                      // the step that is fetched meanwhile
-        const uint32_t next = lds + fill * R::Stage;
-        const int mask = __builtin_amdgcn_readfirstlane(nb < c.kb ? -1 : 0);
         // (no branch around the copies: across one the compiler lets the multiply-adds slide to the step's end, and their operands out of the registers)
-        multiply_step<NT, kSwiglu, kExact>(c, at, at + kWStage, sa, sa_row, sw0, sw1, acc,
-                                           [&](int t) __attribute__((always_inline)) { issue_between<R, kSwiglu>(c, next, nb, t, mask); });
-        fill = fill + 1 == R::NS ? 0 : fill + 1;
-        stage = stage + 1 == R::NS ? 0 : stage + 1;
+        multiply_step<NT, kSwiglu, kExact>(c, ws, xs, sa, sa_row, sw0, sw1, acc,
+                                           [&](int t) __attribute__((always_inline)) { issue_between<R, kSwiglu>(c, lds, wfill, xfill, b, t); });
+        wat = wat + 1 == R::NW ? 0 : wat + 1;
+        xat = xat + 1 == R::NX ? 0 : xat + 1;
+        wfill = wfill + 1 == R::NW ? 0 : wfill + 1;
+        xfill = xfill + 1 == R::NX ? 0 : xfill + 1;
     }
     __syncthreads();   // all reads are done: the ring is the epilogue's
     if constexpr (kSwiglu) store_quantized<NT>(g, c, mt, n0, ring, acc);
