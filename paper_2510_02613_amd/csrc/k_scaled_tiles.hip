@@ -32,7 +32,8 @@ constexpr int kGroup = 4;                      // steps whose scales travel toge
 // which come from memory while the rows are found in L2.
 template <int NT_> struct Ring {
     static constexpr int NT = NT_, BM = NT == 1 ? 32 : (NT + 1) / 2 * 64, XStage = BM * kRowBytes;
-    static constexpr int NW = NT <= 2 ? 4 : NT <= 6 ? 3 : 2, NX = NT == 1 ? 4 : NT <= 4 ? 3 : 2;
+    static constexpr int NW = NT == 1 ? 4 : NT <= 6 ? 3 : 2, NX = NT == 1 ? 4 : NT <= 4 ? 3 : 2;
+    static constexpr bool WeightsFirst = NT <= 2;              // of a step's copies: where everybody waits for the weights
     static constexpr int WP = 4, XP = NT >= 2 ? BM / 64 : 1;     // 1 KB pieces (8 rows) per wavefront and step
     static constexpr int XBase = NW * kWStage, Scales = XBase + NX * XStage, ScaleBytes = 2 * kGroup * BM * 4;
     static constexpr int WScales = Scales + ScaleBytes, WScaleBytes = 2 * 256;
@@ -40,7 +41,7 @@ template <int NT_> struct Ring {
     // before its weights) those behind the rows of b, or with as many stages of both behind its weights.  A wavefront that issues more waits for more.
     static constexpr int P = NT >= 2 ? WP + XP : WP;
     static constexpr int Young = (NX - 2) * P + (NW > NX ? WP : 0);
-    static_assert(NW == NX || NW == NX + 1, "Young");
+    static_assert(NW == NX || (NW == NX + 1 && !WeightsFirst), "Young");
     static_assert(WScales + WScaleBytes <= kLds, "LDS");
 };
 
@@ -84,18 +85,19 @@ __device__ __forceinline__ void wait_loads()
     __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
-// Copy i of this wavefront's for a K-step: rows of step b + NX - 1 first, then weights of step b + NW - 1 (step b is the one that is multiplied meanwhile).
+// Copy i of this wavefront's for a K-step: rows of step b + NX - 1, then weights of step b + NW - 1 (step b is the one that is multiplied meanwhile).
 // A last step that ends inside the block fetches the last 128 columns: what comes before its own is zeroed in LDS before use.  Of a contraction shorter
 // than a block (kShort) chunks behind the row's end repeat the first one, and are zeroed.
 template <typename R, bool kSwiglu, bool kShort, int i>
 __device__ __forceinline__ void issue_copy(const Ctx &c, uint32_t lds, int wstage, int xstage, int b)
 {
-    constexpr bool weights = i >= R::XP;
+    constexpr bool weights = R::WeightsFirst ? i < R::WP : i >= R::XP;
+    constexpr int n = !weights ? (R::WeightsFirst ? i - R::WP : i) : R::WeightsFirst ? i : i - R::XP;    // the how-manieth of its kind
     const int step = b + (weights ? R::NW : R::NX) - 1;
     int mask = step >= 0 && step < c.kb ? -1 : 0;
     if constexpr (!weights && R::NT < 2) mask = c.wave < 4 ? mask : 0;
-    const int pc = weights ? c.wave * R::WP + i - R::XP : c.wave * R::XP + i;
-    uint32_t off = weights ? c.woff[weights ? i - R::XP : 0] : c.xoff[weights ? 0 : i];
+    const int pc = c.wave * (weights ? R::WP : R::XP) + n;
+    uint32_t off = weights ? c.woff[weights ? n : 0] : c.xoff[weights ? 0 : n];
     if (kShort) {
         const int chunk = ((c.lane & 7) ^ swz8(pc * 8 + (c.lane >> 3))) * 16;
         if (chunk >= c.k) off -= chunk;
