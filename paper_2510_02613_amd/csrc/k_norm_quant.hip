@@ -189,7 +189,7 @@ void launch_rows_of(const RowsJob &j, hipStream_t st)
 {
     const int chunks = ((j.cols >> 3) + kWaves * 64 - 1) / (kWaves * 64);
     const dim3 grid(kWaves == 1 ? (j.rows + 3) / 4 : j.rows), block(kWaves == 1 ? 256 : kWaves * 64);
-    if (kWaves < 16 && chunks <= 1) { if constexpr (kWaves < 16) hipLaunchKernelGGL((k_rows<T, kWaves, 1>), grid, block, 0, st, j); }
+    if (chunks <= 1) hipLaunchKernelGGL((k_rows<T, kWaves, 1>), grid, block, 0, st, j);
     else if (kWaves == 1 || chunks <= 2) hipLaunchKernelGGL((k_rows<T, kWaves, 2>), grid, block, 0, st, j);
     else if constexpr (kWaves > 1) hipLaunchKernelGGL((k_rows<T, kWaves, 4>), grid, block, 0, st, j);
 }
@@ -198,9 +198,13 @@ template <typename T>
 void launch_rows_t(const RowsJob &j, hipStream_t st)
 {
     const int chunks = j.cols >> 3;
-    if (chunks <= 128)       launch_rows_of<T, 1>(j, st);
-    else if (chunks <= 1024) launch_rows_of<T, 4>(j, st);
-    else                     launch_rows_of<T, 16>(j, st);
+    // up to two workgroups a compute unit a row is shared out to more wavefronts: less in a row for each of them.  us, norm with all results / quantising, rows
+    // of 7168: 1 row 5.2 / 3.6 -> 3.9 / 2.9, 64 5.7 / 3.9 -> 4.3 / 3.1, 512 8.7 / 4.7 -> 7.9 / 4.1, 1024 13.4 / 6.3 -> 14.0 / 5.7, 2048 21.0 -> 22.8; of
+    // 4096: 1 3.9 -> 3.4, 512 5.9 -> 5.9, 2048 13.4 -> 15.3; of 768: 1 3.5 -> 3.1, 512 4.2 -> 3.7, 2048 5.4 -> 5.6
+    const bool few = j.rows <= 512;
+    if (chunks <= (few ? 64 : 128))        launch_rows_of<T, 1>(j, st);
+    else if (chunks <= (few ? 256 : 1024)) launch_rows_of<T, 4>(j, st);
+    else                                   launch_rows_of<T, 16>(j, st);
 }
 
 }  // namespace

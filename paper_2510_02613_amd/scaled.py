@@ -50,14 +50,17 @@ def _device_of(t: torch.Tensor) -> int:
 
 def _matrix(t: torch.Tensor, shape, dtype, dev: int, what: str):
     """Checks a matrix with contiguous rows; (address, elements from one row to the next)."""
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{what} must be {dtype} {list(shape)}, is {t.dtype} {list(t.shape)}")
-    if t.get_device() != dev:
-        raise ValueError(f"{what} is on {t.device}, not on device {dev}")
-    ld, one = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on device {dev}, is {t.dtype} {list(t.shape)} on {t.device}")
+    if shape[0] > 1:
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1]
+        ld, one = t.stride()
+    else:
+        ld, one = (shape[1] + 15) // 16 * 16, t.stride(1)                       # one row: its stride says nothing
     if one != 1 and shape[1] > 1:
         raise ValueError(f"the rows of {what} must be contiguous")
-    return t.data_ptr(), (ld if shape[0] > 1 else (shape[1] + 15) // 16 * 16)   # one row: its stride says nothing
+    return t.data_ptr(), ld
 
 
 def _whole(t: torch.Tensor, shape, dtype, dev: int, what: str) -> int:
