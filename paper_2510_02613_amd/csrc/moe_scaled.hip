@@ -73,8 +73,9 @@ moe_status_t check_product(int32_t m, int32_t n, int32_t k, const void *a, int64
     return check_scales(a_scale, ld_a_scale, scale_blocks(k), "a_scale");
 }
 
-// How a product of m rows is run: the streaming kernels, or tiles of tile_rows rows.
-struct Plan { bool stream; int tile_rows; };
+// How a product of m rows is run: the streaming kernels, or tiles of tile_rows rows; its workgroups.
+struct Plan { bool stream; int tile_rows; long long groups; };
+constexpr long long kMaxGroups = (1ll << 32) / 512 - 8;   // workgroups of 512 threads that a launch can have
 
 // The faster by what both were measured to take (us).  Streaming: 3 + 0.28 per 32 rows and million weights, with swiglu 7 (a second launch quantises) and
 // 0.24: 4096 x 7168 64 rows 19.3 (tiles 34.9), 128 rows 38 (34.9), 333 rows 89 (36); 7168 x 2048 64 rows 12.8 (13.5), 128 rows 20 (13.7); 1544 x 1424 in
@@ -83,12 +84,14 @@ Plan plan_product(int32_t m, int32_t n, int32_t k, bool swiglu, bool exact)
 {
     const double weights = (swiglu ? 2e-6 : 1e-6) * n * k;
     double best = (swiglu ? 7.0 + 0.24 * weights * ((m + 31) / 32) : 3.0 + 0.28 * weights * ((m + 31) / 32));
-    Plan p = {true, stream_tile_rows(m, n, swiglu)};
+    Plan p = {true, stream_tile_rows(m, n, swiglu), 0};
+    p.groups = (m + p.tile_rows - 1ll) / p.tile_rows * ((n + 15) / 16);      // at most
     const int most = exact ? 128 : 256;
     for (int rows : {32, 64, 128, 192, 256}) {
         if (rows > most) break;
-        const double us = tiles_us((m + rows - 1) / rows, rows, n, k, swiglu, exact);
-        if (us < best) { best = us; p = {false, rows}; }
+        const long long tiles = (m + rows - 1) / rows;
+        const double us = tiles_us(tiles, rows, n, k, swiglu, exact);
+        if (us < best) { best = us; p = {false, rows, tiles * tiles_slices(n, swiglu)}; }
     }
     return p;
 }
@@ -172,6 +175,7 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
     g.out = p->out; g.ld_out = p->ld_out; g.add = p->add; g.ld_add = p->ld_add;
     const bool bf16 = p->out_dtype == MOE_BF16;
     const Plan plan = plan_product(g.m, g.n, g.k, false, !bf16);
+    if (plan.groups > kMaxGroups) return fail(MOE_ERR_UNSUPPORTED, "a result of %d x %d needs more workgroups than a launch can have", g.m, g.n);
     const hipError_t e = plan.stream ? launch_scaled_stream(g, false, bf16, plan.tile_rows, (hipStream_t)hip_stream)
                                      : launch_scaled_tiles(g, bf16 ? TilesOut::bf16 : TilesOut::f32, plan.tile_rows, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
@@ -198,6 +202,7 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
     if (p->workspace_bytes < need) return fail(MOE_ERR_CAPACITY, "workspace has %zu bytes, the product needs %zu", p->workspace_bytes, need);
     SGemm g = product(p->m, p->inter, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
     const Plan plan = plan_product(g.m, g.n, g.k, true, true);
+    if (plan.groups > kMaxGroups) return fail(MOE_ERR_UNSUPPORTED, "a result of %d x %d needs more workgroups than a launch can have", g.m, g.n);
     hipError_t e = hipSuccess;
     if (!plan.stream) {
         g.q = (uint8_t *)p->q; g.qs = p->q_scale; g.ld_q = p->ld_q; g.ld_qs = p->ld_scale;

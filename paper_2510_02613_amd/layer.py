@@ -288,7 +288,7 @@ class MoELayer:
         """A pass of a layer with 8-bit experts for tokens that are in 8 bits already (scaled.rms_norm writes them).  The routing is
         given, or the gate runs on x."""
         T, H, k = xq.shape[0], self.cfg.hidden, self.cfg.top_k
-        assert xq.dtype == torch.float8_e4m3fn and xq.is_contiguous() and xq.shape[1] == H
+        assert xq.dtype == torch.float8_e4m3fn and xq.is_contiguous() and xq.shape[1] == H and xq.device == self.device
         assert x_scale.dtype == torch.float32 and x_scale.is_contiguous() and tuple(x_scale.shape) == (T, (H + 127) // 128) and x_scale.device == xq.device
         assert x is None or (self._is_act(x) and x.is_contiguous() and tuple(x.shape) == (T, H))
         assert (topk_ids is None) == (topk_w is None) and (topk_ids is not None or x is not None)

@@ -191,6 +191,36 @@ def test_swiglu(S, m, inter, k):
     assert torch.isnan(rows[m:].float()).all() and torch.isnan(rows[:, inter:].float()).all() and (scales[m:] == 7).all()
 
 
+@pytest.mark.parametrize("m", [3, 300])
+def test_matmul_of_weights_past_32_bits(S, m):
+    """4.3 GB of weights: rows behind the first 2^32 bytes, streamed and in tiles."""
+    n, k = 66048, 65552
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty(n, k, dtype=E4M3, device="cuda")
+    for at in range(0, n, 4128):      # 0 .. 0x77: finite values
+        w[at:at + 4128].view(torch.uint8).copy_(torch.randint(0, 0x60, (4128, k), dtype=torch.uint8, device="cuda", generator=g))
+    ws = torch.rand(R.blocks(n), R.blocks(k), device="cuda", generator=g) * 1e-3
+    q, scale, a = eight_bit_rows(3, m, k)
+    out = S.matmul(q.cuda(), scale.cuda(), w, ws, out_dtype=torch.float32)
+    cols = [0, 65535, 65536, 65537, 66000, n - 1]
+    wv = torch.stack([w[c].cpu().double() * ws[c // 128].cpu().double().repeat_interleave(128)[:k] for c in cols])
+    y, dy = R.product(a, torch.zeros_like(a), wv)
+    assert ((out[:, cols].cpu().double() - y).abs() <= dy).all()
+
+
+def test_matmul_of_rows_past_32_bits(S):
+    """Rows four million bytes apart, 1100 of them."""
+    m, n, k, ld = 1100, 1536, 1024, 1 << 22
+    q, scale, a = eight_bit_rows(4, m, k)
+    wq, ws, w = eight_bit_weights(5, n, k)
+    wide = torch.empty(m * ld, dtype=torch.uint8, device="cuda").view(E4M3).view(m, ld)[:, :k]
+    wide.view(torch.uint8).copy_(q.view(torch.uint8).cuda())
+    for dtype, fast in ((torch.float32, False), (torch.bfloat16, True)):
+        out = S.matmul(wide, scale.cuda(), wq.cuda(), ws.cuda(), out_dtype=dtype)
+        y, dy = R.product(a, torch.zeros_like(a), w, fast=fast)
+        assert ((out.cpu().double() - y).abs() <= (dy + R.F32 * y.abs()) * (1 + R.BF16) + R.HALF_STEP[dtype] * y.abs()).all()
+
+
 def test_both_forms_of_the_products_run():
     """What the sizes above are for: some are streamed, some go through tiles."""
     from gpu_util import kernels_of

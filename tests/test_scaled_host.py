@@ -95,7 +95,7 @@ PRODUCT = [(dict(m=-1), SHAPE), (dict(k=0), SHAPE), (dict(k=264, ld_a=272), UNSU
 
 @pytest.mark.parametrize("kw,status", PRODUCT + [
     (dict(n=0), SHAPE), (dict(n=(1 << 21) + 1, ld_out=1 << 22), UNSUPPORTED), (dict(out_dtype=3), ARG), (dict(out=0), ARG), (dict(out=0x60004), ARG), (dict(ld_out=252), ARG),
-    (dict(ld_out=260), ARG), (dict(add=0x50002), ARG), (dict(ld_add=4), ARG)])
+    (dict(ld_out=260), ARG), (dict(add=0x50002), ARG), (dict(ld_add=4), ARG), (dict(m=1 << 21, n=1 << 21, ld_out=1 << 21, ld_add=1 << 21), UNSUPPORTED)])
 def test_matmul_refuses(kw, status):
     with pytest.raises(B.MoEError) as e:
         matmul(**kw)()
