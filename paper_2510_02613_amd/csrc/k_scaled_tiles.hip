@@ -159,16 +159,15 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
         return f;
     };
     if (NT <= 2) between(0);
-    typename std::conditional<kExact, Bf16x32, Bytes32>::type wf[4];
+    Bytes32 wf[4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-        const Bytes32 f = fetch(Ws, c.wn * 4 + a);
-        if constexpr (kExact) wf[a].from(f); else wf[a] = f;
-    }
+    for (int a = 0; a < 4; ++a) wf[a] = fetch(Ws, c.wn * 4 + a);
     const auto scale_of = [&](int t) __attribute__((always_inline)) { return sa[((2 * t + c.wm) * 16 + c.l15) * sa_row]; };
     float s[2] = {scale_of(0), 0.f};
     Bytes32 xf[2];
     xf[0] = fetch(Xs, c.wm);
+    Bf16x32 w[kExact ? 4 : 1], x[kExact ? 2 : 1];
+    if constexpr (kExact) x[0].from(xf[0]);
     // two sets of block sums: those of row tile t - 1 are added between the matrix instructions of t.  (Added in front of them, on one set of
     // registers, both wavefronts of a SIMD add at the same time, and the matrix cores wait.)
     f32x4 d[2][4];
@@ -179,14 +178,20 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t + 1 < NT) xf[(t + 1) & 1] = fetch(Xs, 2 * (t + 1) + c.wm);
-        typename std::conditional<kExact, Bf16x32, Bytes32>::type x;
-        if constexpr (kExact) x.from(xf[t & 1]); else x = xf[t & 1];
         const float f0 = s[(t + 1) & 1] * sw0, f1 = kSwiglu ? s[(t + 1) & 1] * sw1 : f0;
         // a wavefront on its matrix instructions goes first: the other one's copies and reads fill the gaps (8192^3 464 -> 450 us, SwiGLU 4096 x 2048 x 7168 208 -> 201)
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            if constexpr (kExact) d[t & 1][a] = multiply_exact(wf[a], x); else d[t & 1][a] = multiply_fast(wf[a], x);
+            if constexpr (kExact) {
+                // the conversions stand between the matrix instructions too: of the weights at their first use, of the next rows under these ones'
+                if (t == 0) w[a].from(wf[a]);
+                d[t & 1][a] = multiply_exact(w[a], x[t & 1]);
+                if (t + 1 < NT && a == 2) { x[(t + 1) & 1].template from_quarter<0>(xf[(t + 1) & 1]); x[(t + 1) & 1].template from_quarter<1>(xf[(t + 1) & 1]); }
+                if (t + 1 < NT && a == 3) { x[(t + 1) & 1].template from_quarter<2>(xf[(t + 1) & 1]); x[(t + 1) & 1].template from_quarter<3>(xf[(t + 1) & 1]); }
+            } else {
+                d[t & 1][a] = multiply_fast(wf[a], xf[t & 1]);
+            }
             if (t > 0) add(t - 1, a, a & 1 ? f1 : f0);
             __builtin_amdgcn_sched_barrier(0);
         }
