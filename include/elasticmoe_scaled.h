@@ -126,7 +126,8 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *args, void *hip_stream
  * type of x and out.  From then on it is a layer as any other: placements (moe_set_expert_map, moe_set_expert_replicas), page pools
  * (slots of 2 I H and H I bytes), profiling, moe_forward and moe_forward_routed, which quantise x.  The rows of h are quantised
  * (from fp32) between the GEMMs; the expert outputs wait for the combine in fp32 or in 16 bits with a scale per 64 columns, so that
- * out is rounded once.  moe_workspace_view's h names the rows of h in 8 bits, its y is not for reading.  MOE_FLAG_FORCE_GENERIC and moe_load_expert are MOE_ERR_UNSUPPORTED on such a layer.
+ * out is rounded once.  moe_workspace_view's h names the rows of h in 8 bits, its y is not for reading.  MOE_FLAG_FORCE_GENERIC and moe_load_expert are MOE_ERR_UNSUPPORTED on such a layer;
+ * moe_forward_static, which knows no layer, takes act_dtype pools only.
  *   MOE_ERR_UNSUPPORTED (beyond moe_layer_create): act_dtype not MOE_BF16, H or I no multiple of 16 or > 32768,
  *   max_tokens * (top_k + n_shared) > 2^21.
  *   moe_load_expert_scaled  moe_load_expert for such a layer: the sources of the weights (16-byte aligned) and of their scales.

@@ -65,7 +65,8 @@ __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t l
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
-// The same for the wavefronts of a mask that is all ones or zero (nothing is copied), without a branch; all lanes are active here.
+// The same for the wavefronts of a mask that is all ones or zero (nothing is copied), without a branch.  Called where all lanes are active, and they are again
+// behind it.
 // kOnce: the line is marked as read once.
 template <bool kOnce>
 __device__ __forceinline__ void dma16_masked(const void *base, uint32_t off, uint32_t lds, int mask)
@@ -435,7 +436,11 @@ __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slice
     const int in_set = (int)(i - (long long)set * slices);
     const int tile = set + in_set % width, n0 = in_set / width * (kSwiglu ? kBN / 2 : kBN);
     MTile mt = {0, tile * tile_rows, min(tile_rows, g.m - tile * tile_rows), 0};
-    if (g.tiles) mt = g.tiles[tile];
+    if (g.tiles) {
+        const MTile m = g.tiles[tile];
+        mt = {__builtin_amdgcn_readfirstlane(m.slot), __builtin_amdgcn_readfirstlane(m.row_begin), __builtin_amdgcn_readfirstlane(m.rows),
+              __builtin_amdgcn_readfirstlane(m.single)};
+    }
 
     Ctx c;
     c.lane = threadIdx.x & 63;

@@ -253,6 +253,39 @@ def test_nan_stays_in_its_row_and_column(S, m):
     assert torch.equal(torch.isnan(out), bad)
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 136, 256), (3001, 1000, 400)])
+def test_rows_behind_the_last_are_left_alone(S, m, n, k):
+    q, scale, _ = eight_bit_rows(5, m, k)
+    wq, ws, _ = eight_bit_weights(6, n, k)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((m + 3, n), 7.0, dtype=dtype, device="cuda")
+        S.matmul(q.cuda(), scale.cuda(), wq.cuda(), ws.cuda(), out=out[:m])
+        assert (out[m:] == 7).all() and not (out[:m] == 7).all(1).any()
+
+
+def test_two_streams_at_once(S):
+    """Products on two streams, each with a workspace of its own, beside each other: what they are one after the other."""
+    sizes = [(9, 768, 2048), (700, 1040, 2064)]
+    args, want = [], []
+    for m, inter, k in sizes:
+        q, scale, _ = eight_bit_rows(m, m, k)
+        w, ws, _ = eight_bit_weights(k, 2 * inter, k, parts=2)
+        args.append([t.cuda() for t in (q, scale, w, ws)])
+        want.append([t.clone() for t in S.swiglu(*args[-1])])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sizes]
+    spaces = [S.swiglu_workspace(*s) for s in sizes]
+    assert spaces[0] is not None and spaces[1] is None
+    got = [[torch.empty_like(t) for t in w] for w in want]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, s, ws, (q, sc) in zip(args, streams, spaces, got):
+            S.swiglu(*a, q=q, scale=sc, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g[0].view(torch.uint8), w[0].view(torch.uint8)) and torch.equal(g[1], w[1])
+
+
 def test_zero_rows_are_a_no_op(S):
     e = lambda *s, dt=E4M3: torch.empty(s, dtype=torch.float32).to(dt).cuda()  # noqa: E731
     assert S.rms_norm(e(0, 128, dt=torch.bfloat16)).out.shape == (0, 128)
