@@ -13,6 +13,8 @@
 // Weight rows are the first operand, so that a lane holds four neighbouring columns of one row of the result.  With swiglu
 // 16 gate rows and the 16 matching up rows alternate: a lane has both values of a column in neighbouring accumulators, and the
 // 128 columns of a tile are one scale group of the 8-bit result, whose maximum is found over the four weight wavefronts through LDS.
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "scaled.h"
@@ -424,22 +426,43 @@ __device__ __forceinline__ void run_nt(int nt, const SGemm &g, Ctx &c, const MTi
 // taken `together` at a time, slice by slice, so that a slice's weights are read by that many workgroups of one XCD while they are in its L2.
 // us, 1, 2, 4 at a time: 8192^3 493, 466, 456; layers, where as many belong together as a slot has tiles: DeepSeek-V3-shaped rank 8192 routed tokens, two
 // tiles a slot, 860, 841, 846, 3000 tokens, one, 467, 497, 516; Qwen3 shape 4096 tokens, one or two, 323, 332, 352.
+//
+// A compute unit runs one workgroup at a time, so that a last round that is not full costs a whole one.  Where it fills half of an XCD's `cus` units or less, the
+// rows of its tiles are shared out to two to four workgroups (parts of whole 32 rows; a row's sums are the same whichever runs it).  cus 0: never.
+// us, whole -> shared out: 8192 x 7168 x 2048 125 -> 121, swiglu of 3000 rows 1408 x 7168 195 -> 158; layers: DeepSeek-V3-shaped rank 3000 tokens 431 -> 407, 8192 799 -> 789,
+// 16 of its experts 6000 tokens 494 -> 463, DeepSeek-V2-Lite shape 1777 tokens 214 -> 203, Qwen3 shape 4096 tokens 322 -> 319, 1500 180 -> 181.
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
-__global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slices, int tile_rows, int together)
+__global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slices, int tile_rows, int together, int cus)
 {
     __shared__ __attribute__((aligned(1024))) char ring[kLds];
     const int tiles = g.tiles ? *g.n_tiles : (g.m + tile_rows - 1) / tile_rows;
-    const long long items = (long long)tiles * slices, share = (items + kXcds - 1) / kXcds;
-    const long long i = (blockIdx.x % kXcds) * share + blockIdx.x / kXcds;
-    if ((long long)(blockIdx.x / kXcds) >= share || i >= items) return;
-    const int set = (int)(i / ((long long)together * slices)) * together, width = min(together, tiles - set);
-    const int in_set = (int)(i - (long long)set * slices);
+    // (32 bits hold the items: a launch has fewer workgroups than that)
+    const unsigned items = (unsigned)tiles * (unsigned)slices, share = (items + kXcds - 1) / kXcds;
+    unsigned j = blockIdx.x / kXcds, parts = 1, part = 0;
+    if (cus > 0) {
+        const unsigned left = share % (unsigned)cus, whole = share - left;
+        if (j >= whole) {
+            parts = left > 0 ? max(1u, min(4u, (unsigned)cus / left)) : 1;
+            part = (j - whole) % parts;
+            j = whole + (j - whole) / parts;
+        }
+    }
+    const unsigned i = (blockIdx.x % kXcds) * share + j;
+    if (j >= share || i >= items) return;
+    const int set = (int)(i / ((unsigned)together * (unsigned)slices)) * together, width = min(together, tiles - set);
+    const int in_set = (int)(i - (unsigned)set * (unsigned)slices);
     const int tile = set + in_set % width, n0 = in_set / width * (kSwiglu ? kBN / 2 : kBN);
     MTile mt = {0, tile * tile_rows, min(tile_rows, g.m - tile * tile_rows), 0};
     if (g.tiles) {
         const MTile m = g.tiles[tile];
         mt = {__builtin_amdgcn_readfirstlane(m.slot), __builtin_amdgcn_readfirstlane(m.row_begin), __builtin_amdgcn_readfirstlane(m.rows),
               __builtin_amdgcn_readfirstlane(m.single)};
+    }
+    if (parts > 1) {
+        const int rows = ((mt.rows + (int)parts - 1) / (int)parts + 31) & ~31, begin = (int)part * rows;
+        if (begin >= mt.rows) return;
+        mt.row_begin += begin;
+        mt.rows = min(rows, mt.rows - begin);
     }
 
     Ctx c;
@@ -454,9 +477,26 @@ __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slice
     c.wsbase = g.ws + (size_t)mt.slot * g.ws_slot + (size_t)nb0 * g.kb;
     c.wsoff = (c.lane & 4) ? (uint32_t)(kSwiglu ? nb : min(1, nb - 1 - nb0)) * (uint32_t)g.kb * 4 : 0;
     c.wide = g.kb % kGroup == 0 && g.ld_as % kGroup == 0 && ((uintptr_t)g.as & 15) == 0;
-    c.once = g.tiles ? mt.single != 0 : tiles == 1;
+    c.once = parts == 1 && (g.tiles ? mt.single != 0 : tiles == 1);
     const int nt = (mt.rows + 31) >> 5;
     run_nt<1, kMaxNT, kSwiglu, kExact, TOut>(nt, g, c, mt, n0, ring);
+}
+
+int tail_parts(long long left, int cus) { return left > 0 ? (int)std::max(1ll, std::min(4ll, cus / left)) : 1; }
+
+// compute units of an XCD of the current device (looked up once per device)
+int cus_per_xcd()
+{
+    static std::atomic<int> cus_of[64] = {};
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 32;
+    n = cus_of[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < kXcds) n = 32 * kXcds;
+        n /= kXcds;
+        cus_of[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }
 
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
@@ -465,7 +505,9 @@ void launch_as(const SGemm &g, int tile_rows, hipStream_t st)
     const int slices = tiles_slices(g.n, kSwiglu);
     const long long tiles = g.tiles ? g.max_tiles : (g.m + tile_rows - 1) / tile_rows;
     const long long share = (tiles * slices + kXcds - 1) / kXcds;
-    hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(share * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.together);
+    const int cus = g.split_tail ? cus_per_xcd() : 0;
+    const long long blocks = !cus ? share : g.tiles ? share + cus : share / cus * cus + (share % cus ? (share % cus) * tail_parts(share % cus, cus) : 0);
+    hipLaunchKernelGGL((k_scaled_tiles<kSwiglu, kExact, kMaxNT, TOut>), dim3((unsigned)(blocks * kXcds)), dim3(kThreads), 0, st, g, slices, tile_rows, g.together, cus);
 }
 
 }  // namespace
@@ -474,11 +516,18 @@ int tiles_slices(int n, bool swiglu) { return (n + (swiglu ? kBN / 2 : kBN) - 1)
 
 // Rounds of the chip times the time of a workgroup: its K-steps and 4 to 6 us for the first copies and the stores.  us a K-step by the tile's 32-row
 // parts, of launches that leave compute units idle .. fill the chip: 1 0.62, 2 0.81, 4 1.0 .. 1.19, 6 1.31 .. 1.55, 8 1.5 .. 2.0; exact products 1 1.08, 2 1.36, 4 1.78.
+// The last round's tiles may be shared out (see the kernel).  (Without a GPU, where refusals are tested: 32 units.)
 double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool exact)
 {
-    const int nt = (tile_rows + 31) / 32;
-    const double step = exact ? (nt <= 1 ? 1.08 : nt <= 2 ? 1.36 : 1.78) : nt <= 1 ? 0.62 : nt <= 2 ? 0.81 : nt <= 4 ? 1.1 : nt <= 6 ? 1.45 : 1.85;
-    return (double)((tiles * tiles_slices(n, swiglu) + 255) / 256) * (scale_blocks(k) * step + 3.5 + 0.25 * nt);
+    const auto workgroup = [&](int rows) {
+        const int nt = (rows + 31) / 32;
+        const double step = exact ? (nt <= 1 ? 1.08 : nt <= 2 ? 1.36 : 1.78) : nt <= 1 ? 0.62 : nt <= 2 ? 0.81 : nt <= 4 ? 1.1 : nt <= 6 ? 1.45 : 1.85;
+        return scale_blocks(k) * step + 3.5 + 0.25 * nt;
+    };
+    constexpr int kCus = 32;
+    const long long share = (tiles * tiles_slices(n, swiglu) + kXcds - 1) / kXcds, left = share % kCus;
+    const int parts = tile_rows > 64 ? tail_parts(left, kCus) : 1;
+    return (double)(share / kCus) * workgroup(tile_rows) + (left ? workgroup((tile_rows + parts - 1) / parts) : 0.0);
 }
 
 hipError_t launch_scaled_tiles(const SGemm &g, TilesOut out, int tile_rows, hipStream_t st)

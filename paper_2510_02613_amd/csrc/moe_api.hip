@@ -688,6 +688,7 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     g1.w_slot = 2 * (size_t)p.I * p.H; g1.ws_slot = 2 * (size_t)scale_blocks(p.I) * scale_blocks(p.H);
     g1.n = p.I; g1.k = p.H; g1.kb = scale_blocks(p.H);
     g1.tiles = p.tiles; g1.n_tiles = p.n_tiles; g1.perm = p.perm; g1.max_tiles = p.max_tiles;
+    g1.split_tail = g2.split_tail = rows > 64.0;
     g1.together = g2.together = std::min(4, std::max(1, (int)(rows / tile_rows + 0.5)));
     g1.out = ws + l->lay.h; g1.ld_out = p.I;
     g1.q = (uint8_t *)(ws + l->lay.hq); g1.qs = (float *)(ws + l->lay.hs); g1.ld_q = p.I; g1.ld_qs = scale_blocks(p.I);

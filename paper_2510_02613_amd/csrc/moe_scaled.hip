@@ -75,7 +75,7 @@ moe_status_t check_product(int32_t m, int32_t n, int32_t k, const void *a, int64
 
 // How a product of m rows is run: the streaming kernels, or tiles of tile_rows rows; its workgroups.
 struct Plan { bool stream; int tile_rows; long long groups; };
-constexpr long long kMaxGroups = (1ll << 32) / 512 - 8;   // workgroups of 512 threads that a launch can have
+constexpr long long kMaxGroups = (1ll << 32) / 512 - 512;   // workgroups of 512 threads that a launch can have, less those that a last round is shared out to
 
 // The faster by what both were measured to take (us).  Streaming: 3 + 0.28 per 32 rows and million weights, with swiglu 7 (a second launch quantises) and
 // 0.24: 4096 x 7168 64 rows 19.3 (tiles 34.9), 128 rows 38 (34.9), 333 rows 89 (36); 7168 x 2048 64 rows 12.8 (13.5), 128 rows 20 (13.7); 1544 x 1424 in
@@ -176,6 +176,7 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
     const bool bf16 = p->out_dtype == MOE_BF16;
     const Plan plan = plan_product(g.m, g.n, g.k, false, !bf16);
     if (plan.groups > kMaxGroups) return fail(MOE_ERR_UNSUPPORTED, "a result of %d x %d needs more workgroups than a launch can have", g.m, g.n);
+    g.split_tail = plan.tile_rows > 64;
     const hipError_t e = plan.stream ? launch_scaled_stream(g, false, bf16, plan.tile_rows, (hipStream_t)hip_stream)
                                      : launch_scaled_tiles(g, bf16 ? TilesOut::bf16 : TilesOut::f32, plan.tile_rows, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
@@ -206,6 +207,7 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
     hipError_t e = hipSuccess;
     if (!plan.stream) {
         g.q = (uint8_t *)p->q; g.qs = p->q_scale; g.ld_q = p->ld_q; g.ld_qs = p->ld_scale;
+        g.split_tail = plan.tile_rows > 64;
         e = launch_scaled_tiles(g, TilesOut::swiglu_exact, plan.tile_rows, (hipStream_t)hip_stream);
     } else {
         g.out = p->workspace; g.ld_out = p->inter;

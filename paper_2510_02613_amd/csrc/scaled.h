@@ -43,6 +43,7 @@ struct SGemm {
     const int32_t *perm;
     int32_t max_tiles;
     int32_t together;             // tiles that share weights and are worked on side by side
+    int32_t split_tail;           // the rows of a last round that is not full may be shared out to more workgroups
     // result rows; with swiglu silu(gate) * up
     void *out;
     int64_t ld_out;

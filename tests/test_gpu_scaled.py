@@ -253,6 +253,20 @@ def test_nan_stays_in_its_row_and_column(S, m):
     assert torch.equal(torch.isnan(out), bad)
 
 
+@pytest.mark.parametrize("m,n,k", [(1000, 1032, 1152), (4500, 2100, 1152), (9000, 4100, 384)])
+def test_a_row_is_the_same_wherever_it_stands(S, m, n, k):
+    """Rows of whole tiles, of the last one and of tiles that several workgroups share: the second half repeats the first."""
+    q, scale, _ = eight_bit_rows(m + k, m // 2, k)
+    q, scale = torch.cat([q.view(torch.uint8)] * 2).view(q.dtype).cuda(), torch.cat([scale] * 2).cuda()
+    wq, ws, _ = eight_bit_weights(n + k, n, k)
+    for dtype in (torch.bfloat16, torch.float32):
+        out = S.matmul(q, scale, wq.cuda(), ws.cuda(), out_dtype=dtype)
+        assert torch.equal(out[:m // 2], out[m // 2:])
+    wq, ws, _ = eight_bit_weights(n, 2 * n - n % 16 * 2, k, parts=2)
+    got = S.swiglu(q, scale, wq.cuda(), ws.cuda())
+    assert torch.equal(got.q[:m // 2].view(torch.uint8), got.q[m // 2:].view(torch.uint8)) and torch.equal(got.scale[:m // 2], got.scale[m // 2:])
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 136, 256), (3001, 1000, 400)])
 def test_rows_behind_the_last_are_left_alone(S, m, n, k):
     q, scale, _ = eight_bit_rows(5, m, k)
