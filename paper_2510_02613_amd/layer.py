@@ -5,6 +5,7 @@ out, and names the stream.  Nothing in this file computes any step of the layer.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -25,6 +26,15 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream], device: torch.device) -> in
     """hipStream_t of `stream`, or of the device's current stream (read as a plain handle: building a Stream object
     costs more than enqueueing a kernel)."""
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+_NO_STREAM = contextlib.nullcontext()
+
+
+def _owned_by(stream: Optional[torch.cuda.Stream]):
+    """What a call on `stream` allocates belongs to that stream.  (A block of the current stream's could still be in use by earlier work of
+    that one, or, dropped on return, be handed to its later work, while the kernels on `stream` read and write it.)"""
+    return _NO_STREAM if stream is None else torch.cuda.stream(stream)
 
 
 class _DeviceSpan:
@@ -111,7 +121,8 @@ class MoELayer:
 
     w13 / w2 are the physical slot pools [S,2I,H] / [S,H,I]; fill or refill slots
     with `load_slot`, then switch placement with `set_expert_map`.  With `scaled` given the experts are held in 8 bits, in
-    those pools (fill them directly, or with `load_expert_async`).
+    those pools (fill them directly, or with `load_expert_async`).  Calls work on `stream` (the current one by default);
+    a result that is not given is allocated as if the call stood under torch.cuda.stream(stream).
     """
 
     def __init__(self, *, hidden, inter, n_experts, top_k, n_slots, max_tokens, act_dtype="bf16",
@@ -244,7 +255,8 @@ class MoELayer:
         assert self._is_act(x) and x.is_contiguous() and x.shape[1] == self.cfg.hidden
         T = x.shape[0]
         if out is None:
-            out = torch.empty_like(x)
+            with _owned_by(stream):
+                out = torch.empty_like(x)
         s = _stream_ptr(stream, self.device)
         B.moe_forward(self.handle, x.data_ptr(), T, out.data_ptr(), int(shared_range[0]),
                       int(shared_range[1]), s, flags)
@@ -259,7 +271,8 @@ class MoELayer:
             raise ValueError("forward_static does not serve layers with 8-bit experts")
         assert x.dtype == self.elt and x.is_contiguous() and x.shape[1] == self.cfg.hidden
         if out is None:
-            out = torch.empty_like(x)
+            with _owned_by(stream):
+                out = torch.empty_like(x)
         s = _stream_ptr(stream, self.device)
         buf = B.MoEBuffers(self.buf.router_w, self.buf.logit_bias, self.buf.select_bias, self.buf.w13, self.buf.w2, 0, 0)
         B.moe_forward_static(self.cfg, buf, self.plain_map[0], self.plain_map[1], x.data_ptr(), x.shape[0], out.data_ptr(),
@@ -276,7 +289,8 @@ class MoELayer:
         assert topk_w.dtype == torch.float32 and topk_w.is_contiguous() and tuple(topk_w.shape) == (T, self.cfg.top_k)
         assert topk_ids.device == x.device and topk_w.device == x.device
         if out is None:
-            out = torch.empty_like(x)
+            with _owned_by(stream):
+                out = torch.empty_like(x)
         s = _stream_ptr(stream, self.device)
         B.moe_forward_routed(self.handle, x.data_ptr(), T, topk_ids.data_ptr(), topk_w.data_ptr(), out.data_ptr(),
                              int(shared_range[0]), int(shared_range[1]), s, flags)
@@ -296,7 +310,8 @@ class MoELayer:
             assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous() and tuple(topk_ids.shape) == (T, k) and topk_ids.device == xq.device
             assert topk_w.dtype == torch.float32 and topk_w.is_contiguous() and tuple(topk_w.shape) == (T, k) and topk_w.device == xq.device
         if out is None:
-            out = torch.empty((T, H), dtype=torch.bfloat16 if x is None else x.dtype, device=xq.device)
+            with _owned_by(stream):
+                out = torch.empty((T, H), dtype=torch.bfloat16 if x is None else x.dtype, device=xq.device)
         assert self._is_act(out) and out.is_contiguous() and tuple(out.shape) == (T, H)
         B.moe_forward_scaled(self.handle, 0 if x is None else x.data_ptr(), xq.data_ptr(), x_scale.data_ptr(), T,
                              0 if topk_ids is None else topk_ids.data_ptr(), 0 if topk_w is None else topk_w.data_ptr(), out.data_ptr(),

@@ -3,6 +3,7 @@ and 128 columns of an activation, one for each block of 128 x 128 of a weight ma
 
 torch is plumbing here: it holds device memory and names the stream.  Every function enqueues its kernels on `stream` (the current
 one of the tensors' device by default) and returns the tensors that hold the results; results that are given are written in place.
+What a call allocates itself, results and workspace, belongs to `stream`, as if the call stood under torch.cuda.stream(stream).
 Matrices are [rows, cols] with contiguous rows; rows may lie further apart (`stride(0)`), weights and their scales are contiguous.
 """
 from __future__ import annotations
@@ -12,6 +13,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as B
+from .layer import _owned_by
 
 BLOCK = 128
 E4M3 = torch.float8_e4m3fn
@@ -87,8 +89,9 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual
     shape, dt = x.shape, x.dtype
     rows, cols = shape
     if sum_out is None and out is None and q is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        sum_out = None if residual is None else torch.empty_like(out)
+        with _owned_by(stream):
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            sum_out = None if residual is None else torch.empty_like(out)
     px, ld_x = _matrix(x, shape, dt, dev, "x")
     pr, ld_r = (0, 0) if residual is None else _matrix(residual, shape, dt, dev, "residual")
     pw = 0 if weight is None else _whole(weight, (cols,), dt, dev, "weight")
@@ -113,10 +116,10 @@ def quantize(x: torch.Tensor, *, block_rows: int = 1, q: Optional[torch.Tensor] 
     shape, dt = x.shape, x.dtype
     rows, cols = shape
     groups = (rows if block_rows == 1 else blocks(rows), blocks(cols))
-    if q is None:
-        q = torch.empty(shape, dtype=E4M3, device=x.device)
-    if scale is None:
-        scale = torch.empty(groups, dtype=torch.float32, device=x.device)
+    if q is None or scale is None:
+        with _owned_by(stream):
+            q = torch.empty(shape, dtype=E4M3, device=x.device) if q is None else q
+            scale = torch.empty(groups, dtype=torch.float32, device=x.device) if scale is None else scale
     px, ld_x = _matrix(x, shape, dt, dev, "x")
     pq, ld_q = _matrix(q, shape, E4M3, dev, "q")
     pc, ld_c = _matrix(scale, groups, torch.float32, dev, "scale")
@@ -137,7 +140,8 @@ def matmul(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: tor
     n = w.shape[0]
     if out is None:
         # rows of the result start on 16 bytes whatever n is
-        out = torch.empty((m, (n + 7) // 8 * 8), dtype=add.dtype if add is not None else out_dtype, device=a.device)[:, :n]
+        with _owned_by(stream):
+            out = torch.empty((m, (n + 7) // 8 * 8), dtype=add.dtype if add is not None else out_dtype, device=a.device)[:, :n]
     dt = out.dtype
     if dt not in _DTYPE:
         raise ValueError("out must be bfloat16 or float32")
@@ -169,14 +173,13 @@ def swiglu(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: tor
             return swiglu(a, a_scale, w, w_scale, q=q, scale=scale, workspace=workspace, stream=stream)
     m, k = a.shape
     inter = w.shape[0] // 2
-    if q is None:
-        q = torch.empty((m, inter), dtype=E4M3, device=a.device)
-    if scale is None:
-        scale = torch.empty((m, blocks(inter)), dtype=torch.float32, device=a.device)
-    if workspace is None:
-        workspace = swiglu_workspace(m, inter, k, a.device)
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("the workspace must be contiguous and on the device of a")
+    if q is None or scale is None or workspace is None:
+        with _owned_by(stream):
+            q = torch.empty((m, inter), dtype=E4M3, device=a.device) if q is None else q
+            scale = torch.empty((m, blocks(inter)), dtype=torch.float32, device=a.device) if scale is None else scale
+            workspace = swiglu_workspace(m, inter, k, a.device) if workspace is None else workspace
     kb, nb = (k + 127) // 128, (inter + 127) // 128
     pa, ld_a = _matrix(a, (m, k), E4M3, dev, "a")
     pas, ld_as = _matrix(a_scale, (m, kb), torch.float32, dev, "a_scale")
