@@ -69,17 +69,18 @@ typedef struct {
 moe_status_t moe_quantize(const moe_quantize_t *args, void *hip_stream);
 
 /*
- * out = a w^T (+ add): 8-bit rows times 8-bit weights.  The 128 products of a scale block are summed by the matrix cores, the blocks'
- * sums times their two scales in fp32; one rounding at the end.  out may be add itself (same address and ld).
- * bf16 results of many rows come from the 8-bit matrix instructions, which drop of eight products what lies 2^-14 below the largest
- * (1.5e-5 to 6e-5 of the result's norm, far below the rounding to bf16); fp32 results, and the 8-bit rows of the SwiGLU product
- * below, from exact products.
- *   MOE_ERR_UNSUPPORTED: k no multiple of 16, m or n > 2^21, rows of a or w of 2^23 bytes or more, ld_a_scale of 2^21 or
+ * out = a w^T (+ add): 8-bit rows times 8-bit weights.  Products are exact, the sums of a scale block's 128 and of the blocks' sums
+ * times their two scales fp32; one rounding at the end.  out may be add itself (same address and ld).
+ * bf16 results may come from the 8-bit matrix instructions, at up to twice the rate for many rows, where the caller asks for it: those drop of
+ * eight products what lies 2^-14 below the largest (1.5e-5 to 6e-5 of the norm of usual results; where large products
+ * cancel, what they leave is lost).  Few rows are streamed with exact products then too: a row may come out differently in calls of different m.
+ *   MOE_ERR_UNSUPPORTED: MOE_FAST_PRODUCTS with fp32 results; k no multiple of 16, m or n > 2^21, rows of a or w of 2^23 bytes or more, ld_a_scale of 2^21 or
  *   more, more tiles than a launch can have workgroups (some 2^39 results).
  */
+#define MOE_FAST_PRODUCTS 0x100
 typedef struct {
     int32_t m, n, k;
-    int32_t out_dtype;      /* moe_dtype_t of add and out */
+    int32_t out_dtype;      /* moe_dtype_t of add and out; MOE_BF16 | MOE_FAST_PRODUCTS: bf16 from the 8-bit instructions */
     const void  *a;         /* [m, k] e4m3, 16-byte aligned rows */
     int64_t ld_a;
     const float *a_scale;   /* [m, ceil(k/128)] */

@@ -533,8 +533,9 @@ double tiles_us(long long tiles, int tile_rows, int n, int k, bool swiglu, bool 
 hipError_t launch_scaled_tiles(const SGemm &g, TilesOut out, int tile_rows, hipStream_t st)
 {
     switch (out) {
-    case TilesOut::bf16:         launch_as<false, false, 8, uint16_t>(g, tile_rows, st); break;
+    case TilesOut::bf16:         launch_as<false, true, 4, uint16_t>(g, tile_rows, st); break;
     case TilesOut::f32:          launch_as<false, true, 4, float>(g, tile_rows, st); break;
+    case TilesOut::fast_bf16:    launch_as<false, false, 8, uint16_t>(g, tile_rows, st); break;
     case TilesOut::block16:      launch_as<false, false, 8, Block16>(g, tile_rows, st); break;
     case TilesOut::swiglu:       launch_as<true, false, 8, float>(g, tile_rows, st); break;
     case TilesOut::swiglu_exact: launch_as<true, true, 4, float>(g, tile_rows, st); break;

@@ -78,8 +78,8 @@ struct Plan { bool stream; int tile_rows; long long groups; };
 constexpr long long kMaxGroups = (1ll << 32) / 512 - 512;   // workgroups of 512 threads that a launch can have, less those that a last round is shared out to
 
 // The faster by what both were measured to take (us).  Streaming: 3 + 0.28 per 32 rows and million weights, with swiglu 7 (a second launch quantises) and
-// 0.24: 4096 x 7168 64 rows 19.3 (tiles 34.9), 128 rows 38 (34.9), 333 rows 89 (36); 7168 x 2048 64 rows 12.8 (13.5), 128 rows 20 (13.7); 1544 x 1424 in
-// fp32 333 rows 8.9 (19.1), 1000 rows 20 (20.1); swiglu 2048 x 7168 128 rows 39 (60), 333 rows 75 (60.7), 1408 x 2048 128 rows 15 (21.2), 333 rows 21.9 (21.3).
+// 0.24: 4096 x 7168 64 rows 19.3 (fast tiles 34.9), 128 rows 38 (fast 34.9), 333 rows 89 (exact 55, fast 36); 7168 x 2048 64 rows 12.8 (fast 13.5), 128 rows
+// 20 (fast 13.7), 333 rows 46 (exact 23, fast 16); 1544 x 1424 in fp32 333 rows 8.9 (19.1), 1000 rows 20 (20.1); swiglu 2048 x 7168 128 rows 39 (60), 333 rows 75 (60.7), 1408 x 2048 128 rows 15 (21.2), 333 rows 21.9 (21.3).
 Plan plan_product(int32_t m, int32_t n, int32_t k, bool swiglu, bool exact)
 {
     const double weights = (swiglu ? 2e-6 : 1e-6) * n * k;
@@ -165,20 +165,23 @@ moe_status_t moe_quantize(const moe_quantize_t *n, void *hip_stream)
 moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *p, void *hip_stream)
 {
     if (!p) return fail(MOE_ERR_ARG, "arguments are NULL");
-    EMOE_TRY(check_dtype(p->out_dtype, "out_dtype"));
+    const bool fast = (p->out_dtype & MOE_FAST_PRODUCTS) != 0;
+    const int32_t dtype = p->out_dtype & ~MOE_FAST_PRODUCTS;
+    EMOE_TRY(check_dtype(dtype, "out_dtype"));
+    if (fast && dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "MOE_FAST_PRODUCTS is for bf16 results");
     EMOE_TRY(check_product(p->m, p->n, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale));
     if (p->m == 0) return MOE_OK;
     if (!p->out) return fail(MOE_ERR_ARG, "out is NULL");
-    EMOE_TRY(check_rows(p->out, p->ld_out, p->n, p->out_dtype, "out"));
-    if (p->add) EMOE_TRY(check_rows(p->add, p->ld_add, p->n, p->out_dtype, "add"));
+    EMOE_TRY(check_rows(p->out, p->ld_out, p->n, dtype, "out"));
+    if (p->add) EMOE_TRY(check_rows(p->add, p->ld_add, p->n, dtype, "add"));
     SGemm g = product(p->m, p->n, p->k, p->a, p->ld_a, p->a_scale, p->ld_a_scale, p->w, p->w_scale);
     g.out = p->out; g.ld_out = p->ld_out; g.add = p->add; g.ld_add = p->ld_add;
-    const bool bf16 = p->out_dtype == MOE_BF16;
-    const Plan plan = plan_product(g.m, g.n, g.k, false, !bf16);
+    const bool bf16 = dtype == MOE_BF16;
+    const Plan plan = plan_product(g.m, g.n, g.k, false, !fast);
     if (plan.groups > kMaxGroups) return fail(MOE_ERR_UNSUPPORTED, "a result of %d x %d needs more workgroups than a launch can have", g.m, g.n);
     g.split_tail = plan.tile_rows > 64;
     const hipError_t e = plan.stream ? launch_scaled_stream(g, false, bf16, plan.tile_rows, (hipStream_t)hip_stream)
-                                     : launch_scaled_tiles(g, bf16 ? TilesOut::bf16 : TilesOut::f32, plan.tile_rows, (hipStream_t)hip_stream);
+                                     : launch_scaled_tiles(g, fast ? TilesOut::fast_bf16 : bf16 ? TilesOut::bf16 : TilesOut::f32, plan.tile_rows, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }

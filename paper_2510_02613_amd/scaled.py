@@ -129,13 +129,14 @@ def quantize(x: torch.Tensor, *, block_rows: int = 1, q: Optional[torch.Tensor] 
 
 
 def matmul(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, add: Optional[torch.Tensor] = None,
-           out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+           out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16, fast: bool = False,
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """a w^T (+ add) of 8-bit rows a [m, k] and 8-bit weights w [n, k]; out may be add itself."""
+    """a w^T (+ add) of 8-bit rows a [m, k] and 8-bit weights w [n, k]; out may be add itself.  fast: bf16 results of many rows
+    from the 8-bit matrix instructions, at up to twice the rate, which drop of eight products what lies 2^-14 below the largest."""
     dev = _device_of(a)
     if dev != _current_device():
         with torch.cuda.device(dev):
-            return matmul(a, a_scale, w, w_scale, add=add, out=out, out_dtype=out_dtype, stream=stream)
+            return matmul(a, a_scale, w, w_scale, add=add, out=out, out_dtype=out_dtype, fast=fast, stream=stream)
     m, k = a.shape
     n = w.shape[0]
     if out is None:
@@ -152,7 +153,7 @@ def matmul(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: tor
     pws = _whole(w_scale, ((n + 127) // 128, kb), torch.float32, dev, "w_scale")
     pad, ld_ad = (0, 0) if add is None else _matrix(add, (m, n), dt, dev, "add")
     po, ld_o = _matrix(out, (m, n), dt, dev, "out")
-    B.moe_scaled_matmul(_pack_matmul(m, n, k, _DTYPE[dt], pa, ld_a, pas, ld_as, pw, pws, pad, ld_ad, po, ld_o),
+    B.moe_scaled_matmul(_pack_matmul(m, n, k, _DTYPE[dt] | (B.MOE_FAST_PRODUCTS if fast else 0), pa, ld_a, pas, ld_as, pw, pws, pad, ld_ad, po, ld_o),
                         _current_stream(dev) if stream is None else stream.cuda_stream)
     return out
 
