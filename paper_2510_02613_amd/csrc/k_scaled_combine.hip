@@ -1,5 +1,6 @@
 // Un-permute and weighted combine of a layer with 8-bit experts: out[t] = sum_j w[t,j] y[inv[t,j]], in selection order (shared experts last, weight 1),
-// in fp32 with one rounding at the end.  y are fp32 rows, or 16-bit rows with a scale per 64 columns (Block16 in scaled.h).
+// in fp32 with one rounding at the end.  y are fp32 rows, or, in passes that take the 8-bit
+// matrix instructions, 16-bit rows with a scale per 64 columns (Block16 in scaled.h).
 //
 // A workgroup owns one token and every gridDim.y-th run of 256 chunks of 8 columns.  Bound by memory: the rows of four assignments are
 // requested before any is added.

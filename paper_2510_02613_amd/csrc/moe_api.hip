@@ -154,7 +154,7 @@ Layout make_layout(const moe_config_t &c, bool tight = false, bool scaled = fals
     L.xs = take(scaled ? 4 * T * scale_blocks(c.hidden) : 0);
     L.hq = take(scaled ? A * c.inter : 0);
     L.hs = take(scaled ? 4 * A * scale_blocks(c.inter) : 0);
-    L.y = take(scaled ? std::max(2 * A, 4 * std::min(A, (size_t)kStreamRows)) * c.hidden : esize(c.act_dtype) * A * c.hidden);
+    L.y = take((scaled ? 4 : esize(c.act_dtype)) * A * c.hidden);   // 8-bit experts: fp32 rows
     L.ys = take(scaled ? 4 * A * scaled_out_groups(c.hidden) : 0);
     // partial sums of split tiles: only layers whose large-tile GEMMs can have contractions long enough to split
     L.has_partials = !scaled && c.act_dtype == MOE_BF16 && c.hidden % 64 == 0 && c.inter % 64 == 0 && (c.hidden >= 4096 || c.inter >= 4096) &&
@@ -663,19 +663,23 @@ moe_status_t moe_workspace_view(const moe_layer_t *l, moe_workspace_view_t *v)
 }
 
 // What is left of a pass of a layer with 8-bit experts: p is filled in but for the tile list's size.
-static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool identity, const void *xq, const float *x_scale, hipStream_t st)
+// fast: the caller takes the 8-bit matrix instructions where the weights are not streamed, and expert outputs in 16 bits.
+static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool identity, bool fast, const void *xq, const float *x_scale, hipStream_t st)
 {
     char *ws = (char *)l->buf.workspace;
     const int resident = l->slots_used - p.n_shared < p.E ? l->slots_used - p.n_shared : p.E;
     const double here = routed ? 1.0 - std::pow(1.0 - (double)resident / p.E, p.k) : 1.0;   // share of all tokens that are sent here
     const double rows = resident > 0 ? (double)p.T * p.k / p.E / here : 0.0;                // of a slot, for an even load
     const long long assigned = (long long)p.T * p.k + (long long)(p.shared_end - p.shared_begin) * p.n_shared;
-    // A handful of tiles leaves most of the chip idle: their weights are streamed by many small workgroups then.  us, streaming -> tiles:
-    // DeepSeek-V3-shaped rank 1 token 34 -> 63, 3 68 -> 69, 4 89 -> 75, with 16 experts 4 tokens 63 -> 68; Qwen3 shape 1 token 29 -> 33, 2 37.5 -> 34.6, 16 of its experts
-    // 4 tokens 25 -> 31; DeepSeek-V2-Lite shape 1 token 34.5 -> 37.4, 2 46 -> 39: 75 workgroups of GEMM-1 is where they meet.
+    // A handful of tiles leaves most of the chip idle: their weights are streamed by many small workgroups then.  us, streaming -> tiles (fast ones):
+    // DeepSeek-V3-shaped rank 1 token 36 -> 83 (67), 3 64 -> 88 (79), 4 97 -> 96 (86), 8 126 -> 116 (110), 32 213 -> 209, with 4 of its experts 70 tokens 67 -> 88 (77), with
+    // two 150 tokens 90 -> 92 (69); Qwen3 shape 1 token 25 -> 38 (35), 2 33 -> 40 (38), 3 42 -> 43 (40), 4 45 -> 43 (41), 16 of its experts 40 tokens 34 -> 40 (36), four
+    // 400 tokens 42 -> 42 (35); DeepSeek-V2-Lite shape 1 token 31 -> 43 (40), 2 42 -> 47 (44), 3 51 -> 48 (45), two of its experts 250 tokens 47 -> 47 (42): 150 workgroups
+    // of GEMM-1 is where they meet, and 75 where no shape loses against the fast ones.
     const double tiles_expected = resident * (1.0 - std::exp(-rows)) * std::ceil(rows / 32.0) + (p.shared_end > p.shared_begin ? p.n_shared * std::ceil((p.shared_end - p.shared_begin) / 32.0) : 0.0);
-    const bool stream = tiles_expected * tiles_slices(p.I, true) < 75.0 && assigned <= kStreamRows;
-    const int tile_rows = stream ? 32 : 256;
+    const bool stream = tiles_expected * tiles_slices(p.I, true) < (fast ? 75.0 : 150.0) && assigned <= kStreamRows;
+    fast = fast && !stream;
+    const int tile_rows = stream ? 32 : fast ? 256 : 128;
     const long long nonempty = assigned < p.S ? assigned : p.S;
     const long long tiles_most = (assigned + tile_rows - 1) / tile_rows + nonempty;
     p.max_tiles = (int)(tiles_most < assigned ? tiles_most : assigned);
@@ -716,12 +720,12 @@ static moe_status_t scaled_pass(moe_layer_t *l, Pass &p, bool routed, bool ident
     mark(MOE_PHASE_GEMM1);
     if (e == hipSuccess && identity) e = launch_identity_experts(p, st);
     if (e == hipSuccess && !identity && !xq) e = launch_rows(x_rows, true, st);
-    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g1, true, false, tile_rows, st) : launch_scaled_tiles(g1, TilesOut::swiglu, tile_rows, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g1, true, false, tile_rows, st) : launch_scaled_tiles(g1, fast ? TilesOut::swiglu : TilesOut::swiglu_exact, tile_rows, st);
     if (e == hipSuccess && !identity && stream) e = launch_rows(h_rows, false, st);
     mark(MOE_PHASE_GEMM2);
-    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g2, false, false, tile_rows, st) : launch_scaled_tiles(g2, TilesOut::block16, tile_rows, st);
+    if (e == hipSuccess && !identity) e = stream ? launch_scaled_stream(g2, false, false, tile_rows, st) : launch_scaled_tiles(g2, fast ? TilesOut::block16 : TilesOut::f32, tile_rows, st);
     mark(MOE_PHASE_COMBINE);
-    if (e == hipSuccess) e = identity ? launch_combine(p, st) : launch_scaled_combine(p, stream ? nullptr : g2.os, st);
+    if (e == hipSuccess) e = identity ? launch_combine(p, st) : launch_scaled_combine(p, fast ? g2.os : nullptr, st);
     mark(MOE_N_PHASES);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "forward launch failed: %s", hipGetErrorString(e));
     if (ev) l->prof_count++;
@@ -740,7 +744,7 @@ static moe_status_t forward_pass(moe_layer_t *l, const void *x, int32_t T, const
     if (T > c.max_tokens) return fail(MOE_ERR_CAPACITY, "T %d exceeds max_tokens %d", T, c.max_tokens);
     if (shared_begin < 0 || shared_begin > shared_end || shared_end > T)
         return fail(MOE_ERR_ARG, "shared range [%d,%d) is not inside [0,%d]", shared_begin, shared_end, T);
-    if (flags & ~(MOE_FLAG_IDENTITY_EXPERTS | MOE_FLAG_FORCE_GENERIC | MOE_FLAG_GATE_TILED | MOE_FLAG_PERMUTE_UNFUSED)) return fail(MOE_ERR_ARG, "unknown flag bits 0x%x", flags);
+    if (flags & ~(MOE_FLAG_IDENTITY_EXPERTS | MOE_FLAG_FORCE_GENERIC | MOE_FLAG_GATE_TILED | MOE_FLAG_PERMUTE_UNFUSED | (l->scaled() ? MOE_FLAG_FAST_PRODUCTS : 0u))) return fail(MOE_ERR_ARG, "unknown flag bits 0x%x", flags);
     if (!l->has_map) return fail(MOE_ERR_MAP, "no expert map installed: call moe_set_expert_map first");
     {   // page pools bound: a page taken from under a slot of the placement in force would fault the pass
         const moe_status_t backed = check_owned_backed(l, l->slot_owner, "the active placement names a slot whose page is gone");
@@ -793,7 +797,7 @@ static moe_status_t forward_pass(moe_layer_t *l, const void *x, int32_t T, const
     // gated passes up to kFusedMaxTokens tokens: the selection kernel ranks the assignments, one more kernel places them
     p.fused_hist = !routed_ids && T <= kFusedMaxTokens && T <= p.logit_tokens && !(flags & MOE_FLAG_PERMUTE_UNFUSED);
     const bool identity = flags & MOE_FLAG_IDENTITY_EXPERTS;
-    if (l->scaled()) return scaled_pass(l, p, routed_ids != nullptr, identity, xq, x_scale, st);
+    if (l->scaled()) return scaled_pass(l, p, routed_ids != nullptr, identity, (flags & MOE_FLAG_FAST_PRODUCTS) != 0, xq, x_scale, st);
     const bool mfma = p.act_bf16 && !(flags & MOE_FLAG_FORCE_GENERIC);
     // bf16 passes: small weight-streaming tasks of one token tile when a slot expects only a handful of rows (tiny; routed: T*k/E on
     // average) and of up to 64 rows for a dozen or two (ring64), the large-tile kernels above that (wide, big), the 128 x 128 kernels for

@@ -142,7 +142,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float v0, float v1, float v2, floa
 }
 // magnitudes are compared as integers: a NaN is then larger than all else and makes its whole group NaN, whatever the order
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// Expert outputs between the second GEMM and the weighted sum: 16-bit whole numbers with one fp32 scale, largest magnitude / 32767, for 64 columns of
+// Expert outputs between the second GEMM and the weighted sum in a pass whose caller takes the 8-bit matrix instructions: 16-bit whole numbers with one fp32 scale, largest magnitude / 32767, for 64 columns of
 // a row.  As many bytes as bf16 and 30 times less rounding (5e-5 of normal values' norm against 1.7e-3): what comes behind, the weighted sum in fp32, is then
 // rounded once, at the end.  A group that holds a NaN or an infinity is NaN throughout.
 struct Block16 { uint16_t v; };

@@ -300,7 +300,7 @@ class MoELayer:
                        topk_ids: Optional[torch.Tensor] = None, topk_w: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        shared_range=(0, 0), flags: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """A pass of a layer with 8-bit experts for tokens that are in 8 bits already (scaled.rms_norm writes them).  The routing is
-        given, or the gate runs on x."""
+        given, or the gate runs on x.  flags: MOE_FLAG_FAST_PRODUCTS takes the 8-bit matrix instructions, as in the other passes of such a layer."""
         T, H, k = xq.shape[0], self.cfg.hidden, self.cfg.top_k
         assert xq.dtype == torch.float8_e4m3fn and xq.is_contiguous() and xq.shape[1] == H and xq.device == self.device
         assert x_scale.dtype == torch.float32 and x_scale.is_contiguous() and tuple(x_scale.shape) == (T, (H + 127) // 128) and x_scale.device == xq.device
