@@ -96,7 +96,8 @@ moe_status_t moe_scaled_matmul(const moe_scaled_matmul_t *args, void *hip_stream
 
 /*
  * The first half of a dense SwiGLU expert: h = silu(a Wg^T) * (a Wu^T), quantised per row and 128 columns from fp32.
- * Few rows, or little weights, go through fp32 rows in the caller's workspace: moe_scaled_swiglu_workspace_bytes of the same sizes (0: none needed).
+ * Few rows, or little weights, go through fp32 rows in the caller's workspace: moe_scaled_swiglu_workspace_bytes of the same sizes (0: none needed;
+ * more rows may need none where fewer need some), or once and for all moe_scaled_swiglu_max_workspace_bytes, which is enough for every m up to max_m.
  * Calls that share a workspace must be ordered against each other (one stream).
  *   MOE_ERR_UNSUPPORTED: as for the product above; inter no multiple of 16 or > 32768.   MOE_ERR_CAPACITY: workspace too small.
  */
@@ -116,6 +117,7 @@ typedef struct {
     size_t  workspace_bytes;
 } moe_scaled_swiglu_t;
 size_t moe_scaled_swiglu_workspace_bytes(int32_t m, int32_t inter, int32_t k);
+size_t moe_scaled_swiglu_max_workspace_bytes(int32_t max_m, int32_t inter, int32_t k);
 moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *args, void *hip_stream);
 
 /*

@@ -32,6 +32,7 @@ EXPORTS = ("moe_workspace_bytes", "moe_layer_create", "moe_set_expert_map", "moe
            "moe_pool_export", "moe_pool_open", "moe_pool_close")
 # and include/elasticmoe_scaled.h
 EXPORTS_SCALED = ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu", "moe_scaled_swiglu_workspace_bytes",
+                  "moe_scaled_swiglu_max_workspace_bytes",
                   "moe_scaled_workspace_bytes", "moe_layer_create_scaled", "moe_load_expert_scaled", "moe_forward_scaled")
 MOE_FAST_PRODUCTS, MOE_FLAG_FAST_PRODUCTS = 0x100, 16
 MOE_IPC_HANDLE_BYTES = 64
@@ -201,6 +202,8 @@ def lib() -> ctypes.CDLL:
                                          ctypes.c_void_p, ctypes.c_uint32]
         L.moe_scaled_swiglu_workspace_bytes.restype = ctypes.c_size_t
         L.moe_scaled_swiglu_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
+        L.moe_scaled_swiglu_max_workspace_bytes.restype = ctypes.c_size_t
+        L.moe_scaled_swiglu_max_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
         L.moe_last_error.restype = ctypes.c_char_p
         L.moe_last_error.argtypes = []
         _lib = L
@@ -442,6 +445,10 @@ def moe_scaled_matmul(args: MoEScaledMatmul, stream: int = 0) -> None:
 
 def moe_scaled_swiglu_workspace_bytes(m: int, inter: int, k: int) -> int:
     return int(lib().moe_scaled_swiglu_workspace_bytes(m, inter, k))
+
+
+def moe_scaled_swiglu_max_workspace_bytes(max_m: int, inter: int, k: int) -> int:
+    return int(lib().moe_scaled_swiglu_max_workspace_bytes(max_m, inter, k))
 
 
 def moe_scaled_swiglu(args: MoEScaledSwiglu, stream: int = 0) -> None:

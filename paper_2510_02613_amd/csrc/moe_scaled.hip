@@ -192,6 +192,17 @@ size_t moe_scaled_swiglu_workspace_bytes(int32_t m, int32_t inter, int32_t k)
     return ((size_t)m * inter * 4 + 255) / 256 * 256;
 }
 
+size_t moe_scaled_swiglu_max_workspace_bytes(int32_t max_m, int32_t inter, int32_t k)
+{
+    if (max_m <= 0 || inter <= 0 || k <= 0 || max_m > kMaxRows || inter > kMaxRows) return 0;
+    // the most rows that are streamed: which form runs is the same for all m with as many parts of 32 rows
+    for (int32_t parts = (max_m + 31) / 32; parts > 0; --parts) {
+        const size_t bytes = moe_scaled_swiglu_workspace_bytes(parts * 32 < max_m ? parts * 32 : max_m, inter, k);
+        if (bytes) return bytes;
+    }
+    return 0;
+}
+
 moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *p, void *hip_stream)
 {
     if (!p) return fail(MOE_ERR_ARG, "arguments are NULL");

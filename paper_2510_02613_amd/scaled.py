@@ -158,9 +158,10 @@ def matmul(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: tor
     return out
 
 
-def swiglu_workspace(m: int, inter: int, k: int, device="cuda") -> Optional[torch.Tensor]:
-    """A workspace for swiglu() of these sizes, or None when it needs none."""
-    n = B.moe_scaled_swiglu_workspace_bytes(m, inter, k)
+def swiglu_workspace(m: int, inter: int, k: int, device="cuda", up_to: bool = False) -> Optional[torch.Tensor]:
+    """A workspace for swiglu() of these sizes, or None when it needs none.  up_to: for any number of rows up to m (a call of m rows may need
+    none where one of fewer needs some)."""
+    n = (B.moe_scaled_swiglu_max_workspace_bytes if up_to else B.moe_scaled_swiglu_workspace_bytes)(m, inter, k)
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
