@@ -127,7 +127,7 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *args, void *hip_stream
  *   w2_scale   [S, ceil(H/128), ceil(I/128)],
  * all of it the caller's, like the rest of buf, and a workspace of moe_scaled_workspace_bytes(cfg).  cfg->act_dtype is MOE_BF16, the
  * type of x and out.  From then on it is a layer as any other: placements (moe_set_expert_map, moe_set_expert_replicas), page pools
- * (slots of 2 I H and H I bytes), profiling, moe_forward and moe_forward_routed, which quantise x.  Products are exact and
+ * (slots of 2 I H and H I bytes; scales stay with the slot's number when pages are exchanged, the caller exchanges them too), profiling, moe_forward and moe_forward_routed, which quantise x.  Products are exact and
  * their sums fp32's, the rows of h are quantised (from fp32) between the GEMMs, the expert outputs wait for the combine in fp32, and out is rounded once.
  *   MOE_FLAG_FAST_PRODUCTS  the caller takes the 8-bit matrix instructions for the passes that do not stream their weights, at up to twice the rate
  *                           for many tokens: those drop of eight products what lies 2^-14 below the largest.  That moves one of some three thousand

@@ -6,7 +6,7 @@ out, and names the stream.  Nothing in this file computes any step of the layer.
 from __future__ import annotations
 
 import contextlib
-from typing import NamedTuple, Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
@@ -44,6 +44,14 @@ class _DeviceSpan:
         self.__cuda_array_interface__ = {"shape": tuple(shape), "typestr": typestr, "data": (ptr, False), "version": 2}
 
 
+_TYPESTR = {torch.int16: "<i2", torch.float32: "<f4", torch.float8_e4m3fn: "|u1"}
+
+
+def _span(ptr: int, shape, elt: torch.dtype, device) -> torch.Tensor:
+    """Device memory at ptr as a tensor of these elements (8-bit floats by way of bytes: the interface has no name for them)."""
+    return torch.as_tensor(_DeviceSpan(ptr, shape, _TYPESTR[elt]), device=device).view(elt)
+
+
 class VirtualPool:
     """A weight pool as one contiguous virtual tensor [n_vslots, *slot_shape] over separately
     allocated physical pages (the library's moe_vpool_* calls).  `tensor` is a torch view of the
@@ -56,9 +64,7 @@ class VirtualPool:
         self.slot_bytes = int(np.prod(self.slot_shape)) * esize
         with torch.cuda.device(self.device):
             self.handle = B.moe_vpool_create(self.slot_bytes, n_vslots)
-        typestr = {torch.int16: "<i2", torch.float32: "<f4"}[elt]
-        self.tensor = torch.as_tensor(_DeviceSpan(B.moe_vpool_base(self.handle), (n_vslots,) + self.slot_shape, typestr),
-                                      device=self.device)
+        self.tensor = _span(B.moe_vpool_base(self.handle), (n_vslots,) + self.slot_shape, elt, self.device)
 
     def page_alloc(self) -> int:
         return B.moe_vpool_page_alloc(self.handle)
@@ -91,8 +97,7 @@ class AttachedPool:
         self.n_vslots, self.slot_shape, self.elt, self.offset = n_vslots, tuple(slot_shape), elt, offset
         with torch.cuda.device(self.device):
             self.ptr = B.moe_pool_open(handle, offset)
-        typestr = {torch.int16: "<i2", torch.float32: "<f4"}[elt]
-        self.tensor = torch.as_tensor(_DeviceSpan(self.ptr, (n_vslots,) + self.slot_shape, typestr), device=self.device)
+        self.tensor = _span(self.ptr, (n_vslots,) + self.slot_shape, elt, self.device)
 
     def close(self) -> None:
         if getattr(self, "ptr", None):
@@ -109,10 +114,12 @@ def export_pool(t: torch.Tensor):
 
 class ScaledExperts(NamedTuple):
     """Weight pools of experts held in 8 bits: float8_e4m3fn [S,2I,H] and [S,H,I] with fp32 scales of their 128 x 128 blocks,
-    [S, 2 ceil(I/128), ceil(H/128)] (the gate rows' blocks, then the up rows') and [S, ceil(H/128), ceil(I/128)]."""
-    w13: torch.Tensor
+    [S, 2 ceil(I/128), ceil(H/128)] (the gate rows' blocks, then the up rows') and [S, ceil(H/128), ceil(I/128)].
+    w13 and w2 may be pools of such elements (VirtualPool, AttachedPool) instead of tensors.  Scales belong to slot numbers: whoever
+    exchanges the pages of two slots exchanges their scales too."""
+    w13: Union[torch.Tensor, VirtualPool, AttachedPool]
     w13_scale: torch.Tensor
-    w2: torch.Tensor
+    w2: Union[torch.Tensor, VirtualPool, AttachedPool]
     w2_scale: torch.Tensor
 
 
@@ -139,6 +146,10 @@ class MoELayer:
                                else B.MOE_GATE_SIGMOID_GROUP_TOPK, n_group, topk_group,
                                int(renormalize), float(routed_scale), n_shared)
         self.act_dtype = act_dtype
+        if scaled is not None:
+            assert w13_pool is None and w2_pool is None, "8-bit pools are given in `scaled`"
+            w13_pool, w2_pool = (p if isinstance(p, (VirtualPool, AttachedPool)) else None for p in (scaled.w13, scaled.w2))
+            scaled = scaled._replace(**{name: pool.tensor for name, pool in (("w13", w13_pool), ("w2", w2_pool)) if pool is not None})
         self.scaled = scaled
         self.elt = torch.int16 if act_dtype == "bf16" else torch.float32
         self.router_w = _dev(router_w, self.device)
@@ -146,7 +157,6 @@ class MoELayer:
         self.select_bias = None if select_bias is None else _dev(np.asarray(select_bias, np.float32), self.device)
         # the pools: plain allocations, or views of virtual pools the caller maps pages under
         if scaled is not None:
-            assert w13_pool is None and w2_pool is None, "8-bit pools are given whole"
             blocks = lambda n: (n + 127) // 128  # noqa: E731
             for t, dt, shape in ((scaled.w13, torch.float8_e4m3fn, (n_slots, 2 * inter, hidden)), (scaled.w2, torch.float8_e4m3fn, (n_slots, hidden, inter)),
                                  (scaled.w13_scale, torch.float32, (n_slots, 2 * blocks(inter), blocks(hidden))),
