@@ -27,7 +27,8 @@ extern "C" {
  *     r = x + residual,   y = r / sqrt(mean(r^2) + eps) * weight
  *     sum = r,   out = y,   (q, q_scale) = y quantised per row and 128 columns.
  * sum and out may each be x or residual themselves (same address and ld).  Any of the three may be left out, not all.
- * The squares are summed in fp32: a row whose sum of squares leaves it is normalised to zeros.
+ * The squares are summed in fp32, of rows whose squares would leave it times a power of two: any finite r has its norm, but for a row of zeros where
+ * eps is 0, which is NaN.  (r itself is fp32: where x + residual overflows, y is NaN.)
  *   MOE_ERR_UNSUPPORTED: cols no multiple of 8 or > 32768, rows > 2^21.
  */
 typedef struct {
