@@ -138,7 +138,7 @@ moe_status_t moe_scaled_swiglu(const moe_scaled_swiglu_t *args, void *hip_stream
  * moe_workspace_view's h names the rows of h in 8 bits, its y is not for reading.  MOE_FLAG_FORCE_GENERIC and moe_load_expert are MOE_ERR_UNSUPPORTED on such a layer;
  * moe_forward_static, which knows no layer, takes act_dtype pools only.
  *   MOE_ERR_UNSUPPORTED (beyond moe_layer_create): act_dtype not MOE_BF16, H or I no multiple of 16 or > 32768,
- *   max_tokens * (top_k + n_shared) > 2^21.
+ *   max_tokens * hidden >= 2^32, max_tokens * (top_k + n_shared) > 2^21.
  *   moe_load_expert_scaled  moe_load_expert for such a layer: the sources of the weights (16-byte aligned) and of their scales.
  *   moe_forward_scaled      a pass for tokens that are in 8 bits already (moe_rms_norm writes them): xq [T,H] e4m3, contiguous and 16-byte
  *                           aligned, x_scale [T, ceil(H/128)] contiguous.  topk_ids and topk_w as in moe_forward_routed, or both NULL:
