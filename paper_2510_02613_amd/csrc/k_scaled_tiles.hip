@@ -1,12 +1,14 @@
-// Block-scaled e4m3 products of many rows: tiles of up to 256 rows times 256 weight rows (with swiglu 128 gate and 128 up rows).
+// Block-scaled e4m3 products of many rows: tiles of up to 128 rows, with the 8-bit matrix instructions 256, times 256 weight rows (with swiglu 128 gate and
+// 128 up rows).
 //
 //   out[r, c] = sum_b as[r, b] ws[c / 128, b] sum_{k in block b} a[r, k] w[c, k]
 //
 // A K-step is one scale block: 128 bytes of every row of the tile, one cache line each.  Both operands travel straight from global
 // memory into an LDS ring (16 bytes per lane, the XOR swizzle of swz8 applied on the global side), together with the step's
 // scales, four steps at a time.  The block's sums come out of the matrix cores with a zero start and are added to the
-// fp32 accumulators times as * ws: one multiply-add per four results beside one matrix instruction per 256, which the other
-// wavefront of the SIMD hides.
+// fp32 accumulators times as * ws: four multiply-adds a lane for the 256 sums of 16 x 16, beside the one 8-bit or four bf16 matrix instructions of the
+// next 16 x 16.  Exact products (through bf16) are bound by the bf16 matrix rate and the conversions, matrix cores busy 40 to 46 % of a prefill's
+// products; a decode batch by its weights (GEMM-1 of a DeepSeek-V3-shaped rank, 64 tokens, 138 us for 0.91 GB; with the 8-bit instructions 134).
 //
 // Workgroup: 8 wavefronts as 2 (rows) x 4 (weights).  Wavefront (wm, wn) owns weight rows [64 wn, 64 wn + 64) and the 16-row tiles
 // wm, wm + 2, ... of the rows.  A tile with fewer rows runs a body for fewer of them, whose ring is deeper.
@@ -182,7 +184,7 @@ __device__ __forceinline__ void multiply_step(const Ctx &c, const char *Ws, cons
     for (int t = 0; t < NT; ++t) {
         if (t + 1 < NT) xf[(t + 1) & 1] = fetch(Xs, 2 * (t + 1) + c.wm);
         const float f0 = s[(t + 1) & 1] * sw0, f1 = kSwiglu ? s[(t + 1) & 1] * sw1 : f0;
-        // a wavefront on its matrix instructions goes first: the other one's copies and reads fill the gaps (8192^3 464 -> 450 us, SwiGLU 4096 x 2048 x 7168 208 -> 201)
+        // a wavefront on its matrix instructions goes first: the other one's copies and reads fill the gaps (8192^3, 8-bit instructions, 464 -> 450 us, SwiGLU 4096 x 2048 x 7168 208 -> 201)
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
@@ -424,13 +426,15 @@ __device__ __forceinline__ void run_nt(int nt, const SGemm &g, Ctx &c, const MTi
 
 // The items of a launch are (tile, slice of the weights); workgroup b works for XCD b % 8, whose share is a run of items.  Tiles are
 // taken `together` at a time, slice by slice, so that a slice's weights are read by that many workgroups of one XCD while they are in its L2.
-// us, 1, 2, 4 at a time: 8192^3 493, 466, 456; layers, where as many belong together as a slot has tiles: DeepSeek-V3-shaped rank 8192 routed tokens, two
-// tiles a slot, 860, 841, 846, 3000 tokens, one, 467, 497, 516; Qwen3 shape 4096 tokens, one or two, 323, 332, 352.
+// us, 1, 2, 4 at a time, exact products (8-bit instructions): 8192^3 975, 935, 926 (509, 464, 454), 8192 x 7168 x 2048 241, 231, 224 (125, 120, 117);
+// layers, where as many belong together as a slot has tiles of 128 (256) rows: DeepSeek-V3-shaped rank 8192 routed tokens, three (one), 1284, 1303, 1277 (818, 785,
+// 787), 3000 tokens, one, 573, 590, 573 (410, 419, 428); Qwen3 shape 4096 tokens, two (one), 493, 493, 503 (313, 326, 355).
 //
 // A compute unit runs one workgroup at a time, so that a last round that is not full costs a whole one.  Where it fills half of an XCD's `cus` units or less, the
 // rows of its tiles are shared out to two to four workgroups (parts of whole 32 rows; a row's sums are the same whichever runs it).  cus 0: never.
-// us, whole -> shared out: 8192 x 7168 x 2048 125 -> 121, swiglu of 3000 rows 1408 x 7168 195 -> 158; layers: DeepSeek-V3-shaped rank 3000 tokens 431 -> 407, 8192 799 -> 789,
-// 16 of its experts 6000 tokens 494 -> 463, DeepSeek-V2-Lite shape 1777 tokens 214 -> 203, Qwen3 shape 4096 tokens 322 -> 319, 1500 180 -> 181.
+// us, whole -> shared out, exact (8-bit): 8192 x 7168 x 2048 227 -> 223 (123 -> 118), 3000 x 1408 x 7168 96 -> 97 (72 -> 49), swiglu of 3000 rows 1408 x 7168 195 -> 158;
+// layers: DeepSeek-V3-shaped rank 3000 tokens 567 -> 577 (427 -> 410), 8192 1212 -> 1225 (798 -> 785), 16 of its experts 6000 tokens 837 -> 819 (491 -> 457),
+// DeepSeek-V2-Lite shape 1777 tokens 320 -> 323 (214 -> 202), Qwen3 shape 4096 tokens 497 -> 492 (312 -> 314).
 template <bool kSwiglu, bool kExact, int kMaxNT, typename TOut>
 __global__ __launch_bounds__(kThreads, 1) void k_scaled_tiles(SGemm g, int slices, int tile_rows, int together, int cus)
 {
