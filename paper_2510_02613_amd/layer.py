@@ -221,13 +221,13 @@ class MoELayer:
         the next set_expert_map waits for it.  8-bit experts come with their scales."""
         if self.scaled is not None:
             for t, pool in ((w13, self.w13), (w2, self.w2), (w13_scale, self.scaled.w13_scale), (w2_scale, self.scaled.w2_scale)):
-                assert t is not None and t.dtype == pool.dtype and t.is_contiguous() and t.shape == pool.shape[1:]
+                assert t is not None and t.dtype == pool.dtype and t.is_contiguous() and t.shape == pool.shape[1:] and t.device == self.device
             B.moe_load_expert_scaled(self.handle, slot, w13.data_ptr(), w13_scale.data_ptr(), w2.data_ptr(), w2_scale.data_ptr(),
                                      copy_stream.cuda_stream, _stream_ptr(serve_stream, self.device), copy_blocks)
             return
         assert w13_scale is None and w2_scale is None
-        assert w13.dtype == self.elt and w13.is_contiguous() and w13.shape == self.slot13
-        assert w2.dtype == self.elt and w2.is_contiguous() and w2.shape == self.slot2
+        assert w13.dtype == self.elt and w13.is_contiguous() and w13.shape == self.slot13 and w13.device == self.device
+        assert w2.dtype == self.elt and w2.is_contiguous() and w2.shape == self.slot2 and w2.device == self.device
         s = _stream_ptr(serve_stream, self.device)
         B.moe_load_expert(self.handle, slot, w13.data_ptr(), w2.data_ptr(), copy_stream.cuda_stream, s,
                           copy_blocks)
@@ -257,12 +257,18 @@ class MoELayer:
         """bf16 rows come as bit patterns (int16); a layer with 8-bit experts takes bfloat16 as well."""
         return t.dtype == self.elt or (self.scaled is not None and t.dtype == torch.bfloat16)
 
+    def _check_rows(self, x: torch.Tensor, out: Optional[torch.Tensor]) -> None:
+        """What the kernels read and write by address: T whole rows on this layer's device, and room for as many."""
+        assert self._is_act(x) and x.is_contiguous() and x.dim() == 2 and x.shape[1] == self.cfg.hidden and x.device == self.device
+        assert out is None or (self._is_act(out) and out.is_contiguous() and out.dim() == 2 and out.shape[0] >= x.shape[0] and
+                               out.shape[1] == self.cfg.hidden and out.device == self.device)
+
     def upload(self, x: np.ndarray) -> torch.Tensor:
         return _dev(x, self.device)
 
     def forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, shared_range=(0, 0),
                 flags: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        assert self._is_act(x) and x.is_contiguous() and x.shape[1] == self.cfg.hidden
+        self._check_rows(x, out)
         T = x.shape[0]
         if out is None:
             with _owned_by(stream):
@@ -279,7 +285,7 @@ class MoELayer:
         experts: that entry takes weights of the activations' type."""
         if self.scaled is not None:
             raise ValueError("forward_static does not serve layers with 8-bit experts")
-        assert x.dtype == self.elt and x.is_contiguous() and x.shape[1] == self.cfg.hidden
+        self._check_rows(x, out)
         if out is None:
             with _owned_by(stream):
                 out = torch.empty_like(x)
@@ -293,7 +299,7 @@ class MoELayer:
                        out: Optional[torch.Tensor] = None, shared_range=(0, 0), flags: int = 0,
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The pass with the routing given (device int32 ids [T,k], float32 weights [T,k]); no gate."""
-        assert self._is_act(x) and x.is_contiguous() and x.shape[1] == self.cfg.hidden
+        self._check_rows(x, out)
         T = x.shape[0]
         assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous() and tuple(topk_ids.shape) == (T, self.cfg.top_k)
         assert topk_w.dtype == torch.float32 and topk_w.is_contiguous() and tuple(topk_w.shape) == (T, self.cfg.top_k)
@@ -314,7 +320,7 @@ class MoELayer:
         T, H, k = xq.shape[0], self.cfg.hidden, self.cfg.top_k
         assert xq.dtype == torch.float8_e4m3fn and xq.is_contiguous() and xq.shape[1] == H and xq.device == self.device
         assert x_scale.dtype == torch.float32 and x_scale.is_contiguous() and tuple(x_scale.shape) == (T, (H + 127) // 128) and x_scale.device == xq.device
-        assert x is None or (self._is_act(x) and x.is_contiguous() and tuple(x.shape) == (T, H))
+        assert x is None or (self._is_act(x) and x.is_contiguous() and tuple(x.shape) == (T, H) and x.device == self.device)
         assert (topk_ids is None) == (topk_w is None) and (topk_ids is not None or x is not None)
         if topk_ids is not None:
             assert topk_ids.dtype == torch.int32 and topk_ids.is_contiguous() and tuple(topk_ids.shape) == (T, k) and topk_ids.device == xq.device
@@ -322,7 +328,7 @@ class MoELayer:
         if out is None:
             with _owned_by(stream):
                 out = torch.empty((T, H), dtype=torch.bfloat16 if x is None else x.dtype, device=xq.device)
-        assert self._is_act(out) and out.is_contiguous() and tuple(out.shape) == (T, H)
+        assert self._is_act(out) and out.is_contiguous() and tuple(out.shape) == (T, H) and out.device == self.device
         B.moe_forward_scaled(self.handle, 0 if x is None else x.data_ptr(), xq.data_ptr(), x_scale.data_ptr(), T,
                              0 if topk_ids is None else topk_ids.data_ptr(), 0 if topk_w is None else topk_w.data_ptr(), out.data_ptr(),
                              int(shared_range[0]), int(shared_range[1]), _stream_ptr(stream, self.device), flags)
