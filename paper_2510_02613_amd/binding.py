@@ -34,6 +34,8 @@ EXPORTS = ("moe_workspace_bytes", "moe_layer_create", "moe_set_expert_map", "moe
 EXPORTS_SCALED = ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu", "moe_scaled_swiglu_workspace_bytes",
                   "moe_scaled_swiglu_max_workspace_bytes",
                   "moe_scaled_workspace_bytes", "moe_layer_create_scaled", "moe_load_expert_scaled", "moe_forward_scaled")
+# and include/elasticmoe_dispatch.h
+EXPORTS_DISPATCH = ("moe_sort_tokens_workspace_bytes", "moe_sort_tokens", "moe_combine_tokens", "moe_combine_tokens_backward")
 MOE_FAST_PRODUCTS, MOE_FLAG_FAST_PRODUCTS = 0x100, 16
 MOE_IPC_HANDLE_BYTES = 64
 MOE_STATIC_SCRATCH_BYTES = 32 << 20
@@ -88,6 +90,27 @@ class MoEScaledSwiglu(ctypes.Structure):
                 ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
                 ("q_scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t)]
+
+
+class MoESortTokens(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("top_k", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+                ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("zero_rest", ctypes.c_int32),
+                ("ids", ctypes.c_void_p), ("expert_map", ctypes.c_void_p), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("rows", ctypes.c_void_p), ("ld_rows", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("source", ctypes.c_void_p),
+                ("row", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class MoECombineTokens(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("top_k", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("row", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64)]
+
+
+class MoECombineTokensBackward(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("top_k", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("grad_out", ctypes.c_void_p), ("ld_grad_out", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
+                ("row", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("n_rows", ctypes.c_void_p),
+                ("grad_y", ctypes.c_void_p), ("ld_grad_y", ctypes.c_int64), ("grad_weights", ctypes.c_void_p)]
 
 
 def packer(struct_type):
@@ -185,7 +208,8 @@ def lib() -> ctypes.CDLL:
         L.moe_ceiling_stream.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
         L.moe_ceiling_tile_stream.restype = ctypes.c_int
         L.moe_ceiling_tile_stream.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p]
-        for name in ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu"):
+        for name in ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu",
+                     "moe_sort_tokens", "moe_combine_tokens", "moe_combine_tokens_backward"):
             getattr(L, name).restype = ctypes.c_int
             # the arguments as one of the structures above (byref), or packed: bytes laid out as the structure, which cost less to make
             getattr(L, name).argtypes = [ctypes.c_void_p, ctypes.c_void_p]
@@ -204,6 +228,8 @@ def lib() -> ctypes.CDLL:
         L.moe_scaled_swiglu_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
         L.moe_scaled_swiglu_max_workspace_bytes.restype = ctypes.c_size_t
         L.moe_scaled_swiglu_max_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
+        L.moe_sort_tokens_workspace_bytes.restype = ctypes.c_size_t
+        L.moe_sort_tokens_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
         L.moe_last_error.restype = ctypes.c_char_p
         L.moe_last_error.argtypes = []
         _lib = L
@@ -453,6 +479,22 @@ def moe_scaled_swiglu_max_workspace_bytes(max_m: int, inter: int, k: int) -> int
 
 def moe_scaled_swiglu(args: MoEScaledSwiglu, stream: int = 0) -> None:
     _check(lib().moe_scaled_swiglu(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_sort_tokens_workspace_bytes(tokens: int, top_k: int, n_groups: int) -> int:
+    return int(lib().moe_sort_tokens_workspace_bytes(tokens, top_k, n_groups))
+
+
+def moe_sort_tokens(args: MoESortTokens, stream: int = 0) -> None:
+    _check(lib().moe_sort_tokens(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_combine_tokens(args: MoECombineTokens, stream: int = 0) -> None:
+    _check(lib().moe_combine_tokens(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_combine_tokens_backward(args: MoECombineTokensBackward, stream: int = 0) -> None:
+    _check(lib().moe_combine_tokens_backward(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_layer_destroy(layer) -> None:
