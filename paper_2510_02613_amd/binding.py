@@ -36,6 +36,8 @@ EXPORTS_SCALED = ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scal
                   "moe_scaled_workspace_bytes", "moe_layer_create_scaled", "moe_load_expert_scaled", "moe_forward_scaled")
 # and include/elasticmoe_dispatch.h
 EXPORTS_DISPATCH = ("moe_sort_tokens_workspace_bytes", "moe_sort_tokens", "moe_combine_tokens", "moe_combine_tokens_backward")
+# and include/elasticmoe_four_bit.h
+EXPORTS_FOUR_BIT = ("moe_four_bit_quantize", "moe_four_bit_matmul", "moe_four_bit_swiglu")
 MOE_FAST_PRODUCTS, MOE_FLAG_FAST_PRODUCTS = 0x100, 16
 MOE_IPC_HANDLE_BYTES = 64
 MOE_STATIC_SCRATCH_BYTES = 32 << 20
@@ -111,6 +113,24 @@ class MoECombineTokensBackward(ctypes.Structure):
                 ("grad_out", ctypes.c_void_p), ("ld_grad_out", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
                 ("row", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("n_rows", ctypes.c_void_p),
                 ("grad_y", ctypes.c_void_p), ("ld_grad_y", ctypes.c_int64), ("grad_weights", ctypes.c_void_p)]
+
+
+class MoEFourBitQuantize(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64), ("scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64),
+                ("values", ctypes.c_void_p), ("ld_values", ctypes.c_int64)]
+
+
+class MoEFourBitMatmul(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32), ("groups", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("ld_a", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("add", ctypes.c_void_p), ("ld_add", ctypes.c_int64), ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64)]
+
+
+class MoEFourBitSwiglu(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int32), ("inter", ctypes.c_int32), ("k", ctypes.c_int32), ("groups", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("ld_a", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64)]
 
 
 def packer(struct_type):
@@ -209,7 +229,8 @@ def lib() -> ctypes.CDLL:
         L.moe_ceiling_tile_stream.restype = ctypes.c_int
         L.moe_ceiling_tile_stream.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p]
         for name in ("moe_rms_norm", "moe_quantize", "moe_scaled_matmul", "moe_scaled_swiglu",
-                     "moe_sort_tokens", "moe_combine_tokens", "moe_combine_tokens_backward"):
+                     "moe_sort_tokens", "moe_combine_tokens", "moe_combine_tokens_backward",
+                     "moe_four_bit_quantize", "moe_four_bit_matmul", "moe_four_bit_swiglu"):
             getattr(L, name).restype = ctypes.c_int
             # the arguments as one of the structures above (byref), or packed: bytes laid out as the structure, which cost less to make
             getattr(L, name).argtypes = [ctypes.c_void_p, ctypes.c_void_p]
@@ -495,6 +516,18 @@ def moe_combine_tokens(args: MoECombineTokens, stream: int = 0) -> None:
 
 def moe_combine_tokens_backward(args: MoECombineTokensBackward, stream: int = 0) -> None:
     _check(lib().moe_combine_tokens_backward(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_four_bit_quantize(args: MoEFourBitQuantize, stream: int = 0) -> None:
+    _check(lib().moe_four_bit_quantize(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_four_bit_matmul(args: MoEFourBitMatmul, stream: int = 0) -> None:
+    _check(lib().moe_four_bit_matmul(args if type(args) is bytes else ctypes.byref(args), stream))
+
+
+def moe_four_bit_swiglu(args: MoEFourBitSwiglu, stream: int = 0) -> None:
+    _check(lib().moe_four_bit_swiglu(args if type(args) is bytes else ctypes.byref(args), stream))
 
 
 def moe_layer_destroy(layer) -> None:

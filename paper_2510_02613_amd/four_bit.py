@@ -1,0 +1,130 @@
+"""Experts held in 4 bits, over torch tensors: e2m1 values, two a byte, with a power of two (e8m0) for each row and 32 columns.
+
+torch is plumbing here: it holds device memory and names the stream.  Every function enqueues its kernel on `stream` (the current one of the
+tensors' device by default) and returns the tensors that hold the results; results that are given are written in place.  What a call allocates
+itself belongs to `stream`.  Matrices are [rows, cols] with contiguous rows that start on 16 bytes; rows may lie further apart (`stride(0)`); weights
+are contiguous, [n, k / 2] or, for sorted rows, [groups, n, k / 2], their powers [..., n, k / 32].  The bytes may be torch.uint8 or the types
+that name them, torch.float4_e2m1fn_x2 and torch.float8_e8m0fnu.
+
+The products are for serving: they have no gradient, and refuse tensors that ask for one while grad mode is on.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding as B
+from .layer import _owned_by
+from .scaled import _DTYPE, _current_device, _current_stream, _device_of, _matrix, _whole
+
+GROUP = 32
+_CODES = (torch.uint8, torch.float4_e2m1fn_x2)
+_POWERS = (torch.uint8, torch.float8_e8m0fnu)
+
+
+class FourBit(NamedTuple):
+    """A 4-bit matrix: element (i, j) stands for the e2m1 value in half j % 2 of q[i, j // 2], times 2^(scale[i, j // 32] - 127)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+
+
+_pack_quantize, _pack_matmul = B.packer(B.MoEFourBitQuantize), B.packer(B.MoEFourBitMatmul)
+_pack_swiglu = B.packer(B.MoEFourBitSwiglu)
+
+
+def _one_of(t: torch.Tensor, dtypes, what: str):
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, is {t.dtype}")
+    return t.dtype
+
+
+def _no_gradient(*tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
+
+
+def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> FourBit:
+    """x [rows, cols] in 4 bits; values, where given, gets the numbers that they stand for, in x's type (it may be x itself)."""
+    dev = _device_of(x)
+    if dev != _current_device():      # kernels run on the tensors' device, whichever is current
+        with torch.cuda.device(dev):
+            return quantize(x, q=q, scale=scale, values=values, stream=stream)
+    _no_gradient(x, values)
+    if x.dim() != 2 or x.dtype not in _DTYPE:
+        raise ValueError("x must be a bfloat16 or float32 matrix")
+    rows, cols = x.shape
+    if q is None or scale is None:
+        with _owned_by(stream):
+            q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device) if q is None else q
+            scale = torch.empty((rows, cols // GROUP), dtype=torch.uint8, device=x.device) if scale is None else scale
+    px, ld_x = _matrix(x, (rows, cols), x.dtype, dev, "x")
+    pq, ld_q = _matrix(q, (rows, cols // 2), _one_of(q, _CODES, "q"), dev, "q")
+    ps, ld_s = _matrix(scale, (rows, cols // GROUP), _one_of(scale, _POWERS, "scale"), dev, "scale")
+    pv, ld_v = (0, 0) if values is None else _matrix(values, (rows, cols), x.dtype, dev, "values")
+    B.moe_four_bit_quantize(_pack_quantize(rows, cols, _DTYPE[x.dtype], px, ld_x, pq, ld_q, ps, ld_s, pv, ld_v),
+                            _current_stream(dev) if stream is None else stream.cuda_stream)
+    return FourBit(q, scale)
+
+
+def _product(a, w, w_scale, offsets, add, out, out_dtype, stream, dev, swiglu):
+    """Checks both products' arguments; (m, result columns, k, groups, dtype, addresses and strides, out)."""
+    _no_gradient(a, add, out)
+    if a.dim() != 2:
+        raise ValueError("a must be a matrix")
+    m, k = a.shape
+    if offsets is None:
+        if w.dim() != 2:
+            raise ValueError("w must be [n, k / 2] without offsets")
+        groups, n = 1, w.shape[0]
+        po, lead = 0, (n,)
+    else:
+        if w.dim() != 3:
+            raise ValueError("w must be [groups, n, k / 2] with offsets")
+        groups, n = w.shape[0], w.shape[1]
+        po, lead = _whole(offsets, (groups + 1,), torch.int32, dev, "offsets"), (groups, n)
+    cols = n // 2 if swiglu else n
+    if swiglu and n % 2:
+        raise ValueError("w must hold as many gate rows as up rows")
+    if out is None:
+        # rows of the result start on 16 bytes whatever n is; those in no group are zeros
+        with _owned_by(stream):
+            make = torch.empty if offsets is None else torch.zeros
+            out = make((m, (cols + 7) // 8 * 8), dtype=add.dtype if add is not None else out_dtype, device=a.device)[:, :cols]
+    dt = out.dtype
+    if dt not in _DTYPE:
+        raise ValueError("out must be bfloat16 or float32")
+    pa, ld_a = _matrix(a, (m, k), torch.bfloat16, dev, "a")
+    pw = _whole(w, lead + (k // 2,), _one_of(w, _CODES, "w"), dev, "w")
+    ps = _whole(w_scale, lead + (k // GROUP,), _one_of(w_scale, _POWERS, "w_scale"), dev, "w_scale")
+    pd, ld_d = (0, 0) if add is None else _matrix(add, (m, cols), dt, dev, "add")
+    pt, ld_t = _matrix(out, (m, cols), dt, dev, "out")
+    return m, cols, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t, out
+
+
+def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+           out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """a w^T (+ add) of bf16 rows a [m, k] and 4-bit weights; out may be add itself.  offsets (int32 [groups + 1], as sort_tokens makes them): rows
+    offsets[g] .. offsets[g + 1] - 1 take w[g]; rows in no group are not touched, zeros where the call makes the result."""
+    dev = _device_of(a)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return matmul(a, w, w_scale, offsets=offsets, add=add, out=out, out_dtype=out_dtype, stream=stream)
+    m, n, k, groups, dt, pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t, out = _product(a, w, w_scale, offsets, add, out, out_dtype, stream, dev, False)
+    B.moe_four_bit_matmul(_pack_matmul(m, n, k, groups, dt, pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t),
+                          _current_stream(dev) if stream is None else stream.cuda_stream)
+    return out
+
+
+def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+           out_dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """silu(a Wg^T) * (a Wu^T); w [2 inter, k / 2] (with offsets [groups, 2 inter, k / 2]) holds the gate rows, then the up rows."""
+    dev = _device_of(a)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return swiglu(a, w, w_scale, offsets=offsets, out=out, out_dtype=out_dtype, stream=stream)
+    m, inter, k, groups, dt, pa, ld_a, po, pw, ps, _, _, pt, ld_t, out = _product(a, w, w_scale, offsets, None, out, out_dtype, stream, dev, True)
+    B.moe_four_bit_swiglu(_pack_swiglu(m, inter, k, groups, dt, pa, ld_a, po, pw, ps, pt, ld_t),
+                          _current_stream(dev) if stream is None else stream.cuda_stream)
+    return out
