@@ -6,7 +6,6 @@
 namespace emoe {
 
 constexpr int kFourGroup = 32;            // columns that share a power of two: 16 bytes of a row
-constexpr int kFourStep = 128;            // columns of a K-step: 64 bytes of a weight row
 
 struct FourRows {
     int32_t rows, cols;
@@ -24,12 +23,15 @@ struct FourGemm {
     const uint8_t *w, *ws;
     int32_t m, n, k, groups;
     const int32_t *offsets;               // NULL: all rows are group 0's
+    int32_t sparse;                       // many groups may have no rows
     const void *add;
     int64_t ld_add;
     void *out;
     int64_t ld_out;
 };
 bool four_product_fits(const FourGemm &g);    // its workgroups are as many as a launch can have
-hipError_t launch_four_product(const FourGemm &g, bool swiglu, bool out_bf16, hipStream_t st);
+hipError_t launch_four_matmul(const FourGemm &g, bool out_bf16, hipStream_t st);
+hipError_t launch_four_swiglu(const FourGemm &g, bool out_bf16, hipStream_t st);
+constexpr long long kMostThreads = (1ll << 32) - 1;        // of a launch
 
 }  // namespace emoe

@@ -25,6 +25,7 @@ moe_status_t fail(moe_status_t st, const char *fmt, ...)
 constexpr int32_t kMost = 1 << 21;
 constexpr int32_t kMaxGroups = 2047;            // as many as a layer has slots
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxRowStride = 1 << 24;      // of the rows of a: a tile of them is addressed with 32 bits
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
@@ -58,6 +59,7 @@ moe_status_t check_product(int32_t m, int32_t cols, int32_t w_rows, int32_t k, i
     if (!aligned(offsets, 4)) return fail(MOE_ERR_ARG, "offsets must be 4-byte aligned");
     if (m == 0) return MOE_OK;
     EMOE_TRY(check_rows(a, ld_a, k, MOE_BF16, "a"));
+    if (ld_a >= kMaxRowStride) return fail(MOE_ERR_UNSUPPORTED, "ld of a is %d or larger", (int)kMaxRowStride);
     return check_rows(out, ld_out, cols, out_dtype, "out");
 }
 
@@ -98,10 +100,10 @@ moe_status_t moe_four_bit_matmul(const moe_four_bit_matmul_t *p, void *hip_strea
     if (p->add) EMOE_TRY(check_rows(p->add, p->ld_add, p->n, p->out_dtype, "add"));
     FourGemm g = {};
     g.a = (const uint16_t *)p->a; g.ld_a = p->ld_a; g.w = (const uint8_t *)p->w; g.ws = (const uint8_t *)p->w_scale;
-    g.m = p->m; g.n = p->n; g.k = p->k; g.groups = p->groups; g.offsets = p->offsets;
+    g.m = p->m; g.n = p->n; g.k = p->k; g.groups = p->groups; g.offsets = p->offsets; g.sparse = p->groups > 2 * p->m;
     g.add = p->add; g.ld_add = p->ld_add; g.out = p->out; g.ld_out = p->ld_out;
     if (!four_product_fits(g)) return fail(MOE_ERR_UNSUPPORTED, "n * groups: more tiles than a launch can have workgroups");
-    const hipError_t e = launch_four_product(g, false, p->out_dtype == MOE_BF16, (hipStream_t)hip_stream);
+    const hipError_t e = launch_four_matmul(g, p->out_dtype == MOE_BF16, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }
@@ -114,10 +116,10 @@ moe_status_t moe_four_bit_swiglu(const moe_four_bit_swiglu_t *p, void *hip_strea
     if (p->m == 0) return MOE_OK;
     FourGemm g = {};
     g.a = (const uint16_t *)p->a; g.ld_a = p->ld_a; g.w = (const uint8_t *)p->w; g.ws = (const uint8_t *)p->w_scale;
-    g.m = p->m; g.n = p->inter; g.k = p->k; g.groups = p->groups; g.offsets = p->offsets;
+    g.m = p->m; g.n = p->inter; g.k = p->k; g.groups = p->groups; g.offsets = p->offsets; g.sparse = p->groups > 2 * p->m;
     g.out = p->out; g.ld_out = p->ld_out;
     if (!four_product_fits(g)) return fail(MOE_ERR_UNSUPPORTED, "inter * groups: more tiles than a launch can have workgroups");
-    const hipError_t e = launch_four_product(g, true, p->out_dtype == MOE_BF16, (hipStream_t)hip_stream);
+    const hipError_t e = launch_four_swiglu(g, p->out_dtype == MOE_BF16, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(MOE_ERR_HIP, "product launch failed: %s", hipGetErrorString(e));
     return MOE_OK;
 }

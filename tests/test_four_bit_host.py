@@ -70,7 +70,7 @@ def test_quantize_refuses(kw, status):
 
 PRODUCT = [(dict(m=-1), SHAPE), (dict(k=0), SHAPE), (dict(k=272, ld_a=272), UNSUPPORTED), (dict(k=(1 << 21) + 32), UNSUPPORTED), (dict(m=(1 << 21) + 1), UNSUPPORTED), (dict(groups=0), SHAPE),
            (dict(groups=2048), UNSUPPORTED), (dict(offsets=0), ARG), (dict(offsets=0x20002), ARG), (dict(out_dtype=2), ARG), (dict(a=0), ARG), (dict(a=0x10008), ARG), (dict(ld_a=248), ARG),
-           (dict(ld_a=260), ARG), (dict(w=0), ARG), (dict(w=0x30008), ARG), (dict(w_scale=0), ARG), (dict(out=0), ARG), (dict(out=0x60004), ARG), (dict(ld_out=96), ARG), (dict(ld_out=100), ARG)]
+           (dict(ld_a=260), ARG), (dict(ld_a=1 << 24), UNSUPPORTED), (dict(w=0), ARG), (dict(w=0x30008), ARG), (dict(w_scale=0), ARG), (dict(out=0), ARG), (dict(out=0x60004), ARG), (dict(ld_out=96), ARG), (dict(ld_out=100), ARG)]
 
 
 @pytest.mark.parametrize("kw,status", PRODUCT + [
