@@ -63,7 +63,7 @@ __device__ __forceinline__ int nth_group(const FourGemm &g, int n, int &lo, int 
 
 // kWhole: k is whole lines.  kDirect: powers a line at a time, straight from memory.
 template <bool kSwiglu, int NW, int KW, int MT, int WT, int D, int KC, int kWavesPerSimd, bool kDirect, bool kWhole, typename TOut>
-__global__ __launch_bounds__(NW * KW * 64) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd, kWavesPerSimd))) void k_four_rows(FourGemm g, int slices, int row_tiles)
+__global__ __launch_bounds__(NW * KW * 64) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd, kWavesPerSimd))) void k_four_rows(FourGemm g, int slices, int row_tiles, int together)
 {
     constexpr int LT = kSwiglu ? 2 * WT : WT, W = NW * KW, kThreads = W * 64;
     constexpr int XJ = KC ? MT * 2 * KC / kThreads : 1;                 // 16-byte pieces of a chunk's rows a thread
@@ -74,8 +74,9 @@ __global__ __launch_bounds__(NW * KW * 64) __attribute__((amdgpu_waves_per_eu(kW
     const int l15 = lane & 15, quad = lane >> 4, kw = wave % KW, nw = wave / KW;
     char *ss = lds + wave * (LT * 16 * kPowers), *xs = lds + (kDirect ? 0 : W * LT * 16 * kPowers);
 
-    // eight slices' row tiles one after the other: those of a slice, which read the same weights, run on one XCD (workgroup b on XCD b mod 8) at about one time
-    const int at = blockIdx.x / (8 * row_tiles) * 8 + blockIdx.x % 8, first_tile = blockIdx.x / 8 % row_tiles;
+    // `together` slices' row tiles one after the other (a multiple of eight, so that a slice's tiles run on one XCD: workgroup b on XCD b mod 8)
+    const int turn = blockIdx.x / (together * row_tiles), in_turn = blockIdx.x - turn * together * row_tiles;
+    const int first_tile = in_turn / together, at = turn * together + in_turn - first_tile * together;
     const int slice = at % slices, n0 = (slice * NW + nw) * WT * 16;
     int lo, hi;
     const int group = nth_group(g, at / slices, lo, hi);
@@ -342,10 +343,14 @@ hipError_t launch_whole(const FourGemm &g, int row_tiles, hipStream_t st)
     static const hipError_t ready = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds);
     if (ready != hipSuccess) return ready;
     const int slices = slices_of(g, NW * WT * 16);
-    const long long units = ((long long)slices * groups_of(g) + 7) / 8 * 8, most = kMostThreads / (NW * KW * 64) / units;
+    // A slice's row tiles read the same weights and run side by side.  Of sorted rows nobody knows which tiles have none: those workgroups end at once, and
+    // come last.  Between the others they upset how these are dealt out to the chip (in turn with eight others 309 us for 163, with 264 169 for 102).
+    const long long all = ((long long)slices * groups_of(g) + 7) / 8 * 8;
+    const int together = !g.offsets ? 8 : (int)all;
+    const long long units = (all + together - 1) / together * together, most = kMostThreads / (NW * KW * 64) / units;
     // workgroups go on to further row tiles of theirs where a launch could not have one for each
     const int tiles = (int)(most < row_tiles ? most : row_tiles);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(units * tiles)), dim3(NW * KW * 64), (lds_of<kSwiglu, NW, KW, MT, WT, KC, kDirect>(g)), st, g, slices, tiles);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(units * tiles)), dim3(NW * KW * 64), (lds_of<kSwiglu, NW, KW, MT, WT, KC, kDirect>(g)), st, g, slices, tiles, together);
     return hipGetLastError();
 }
 template <bool kSwiglu, int NW, int KW, int MT, int WT, int D, int KC, int kOcc, bool kDirect, typename TOut>
@@ -358,8 +363,9 @@ hipError_t launch_as(const FourGemm &g, int row_tiles, hipStream_t st)
 int rows_each(const FourGemm &g) { return (g.m + groups_of(g) - 1) / groups_of(g); }
 int row_tiles(const FourGemm &g, int rows)
 {
-    const int tiles = (rows_each(g) + rows - 1) / rows;
-    return g.offsets && tiles > 8 ? 8 : tiles;                   // of groups nobody knows which have more: their workgroups go on
+    if (!g.offsets) return (g.m + rows - 1) / rows;
+    const int tiles = (rows_each(g) * 3 / 2 + rows - 1) / rows;  // some groups have more than others; the workgroups of those with still more go on
+    return tiles < 1 ? 1 : tiles > 8 ? 8 : tiles;
 }
 long long workgroups(const FourGemm &g, int cols, int rows) { return (long long)slices_of(g, cols) * groups_of(g) * row_tiles(g, rows); }
 

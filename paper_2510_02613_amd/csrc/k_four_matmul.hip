@@ -4,25 +4,22 @@
 namespace emoe {
 namespace {
 
-constexpr int kEnough = 200;             // workgroups that fill the chip
-
 template <typename TOut>
 hipError_t launch(const FourGemm &g, hipStream_t st)
 {
-    const int each = rows_each(g);
+    const int each = rows_each(g), many = g.offsets ? 128 : 64;
     const bool brief = g.k <= 1024;      // powers a line at a time
-    if (g.m > 16) {
-        if (each > 64 && workgroups(g, 256, 64) >= kEnough) return launch_as<false, 8, 1, 4, 2, 1, 256, 2, false, TOut>(g, row_tiles(g, 64), st);
-        if (each > 16 && workgroups(g, 128, 32) >= kEnough) {
-            if (brief) return launch_as<false, 4, 1, 2, 2, 1, 256, 3, true, TOut>(g, row_tiles(g, 32), st);
-            return launch_as<false, 4, 1, 2, 2, 1, 256, 3, false, TOut>(g, row_tiles(g, 32), st);
-        }
-        if (each <= 16 && workgroups(g, 256, 16) >= kEnough) {
-            if (brief) return launch_as<false, 8, 1, 1, 2, 1, 512, 4, true, TOut>(g, row_tiles(g, 16), st);
-            return launch_as<false, 8, 1, 1, 2, 1, 512, 4, false, TOut>(g, row_tiles(g, 16), st);
-        }
-        if (workgroups(g, 64, 16) >= kEnough) return launch_as<false, 4, 2, 1, 1, 1, 1024, 2, true, TOut>(g, row_tiles(g, 16), st);
+    if (each > many && workgroups(g, 256, 64) >= 200) return launch_as<false, 8, 1, 4, 2, 1, 256, 2, false, TOut>(g, row_tiles(g, 64), st);
+    if (each > 16 && workgroups(g, 128, 32) >= 300) {
+        if (brief) return launch_as<false, 4, 1, 2, 2, 1, 256, 3, true, TOut>(g, row_tiles(g, 32), st);
+        return launch_as<false, 4, 1, 2, 2, 1, 256, 3, false, TOut>(g, row_tiles(g, 32), st);
     }
+    if (each <= 16 && workgroups(g, 256, 16) >= 300) {
+        if (brief) return launch_as<false, 8, 1, 1, 2, 1, 512, 4, true, TOut>(g, row_tiles(g, 16), st);
+        return launch_as<false, 8, 1, 1, 2, 1, 512, 4, false, TOut>(g, row_tiles(g, 16), st);
+    }
+    if (workgroups(g, 128, 16) >= 140) return launch_as<false, 8, 1, 1, 1, 1, 1024, 4, false, TOut>(g, row_tiles(g, 16), st);
+    if (workgroups(g, 64, 16) >= 200) return launch_as<false, 4, 2, 1, 1, 1, 1024, 2, true, TOut>(g, row_tiles(g, 16), st);
     if (lds_of<false, 1, 8, 1, 2, 0, true>(g) <= kMostLds / 2) return launch_as<false, 1, 8, 1, 2, 1, 0, 2, true, TOut>(g, row_tiles(g, 16), st);
     return launch_as<false, 1, 8, 1, 2, 1, 2048, 2, true, TOut>(g, row_tiles(g, 16), st);
 }
