@@ -16,6 +16,8 @@
 // Their powers are read a line's eight at a time, or, where rows are long, 64 at a time by way of LDS: eight at a time the lines of the powers, of which a
 // step needs a sixteenth, push each other out of the first cache (106 us -> 87).
 #pragma once
+#include <atomic>
+
 #include "four_tiles.h"
 
 namespace emoe {
@@ -335,13 +337,29 @@ size_t lds_of(const FourGemm &g)
     return (kDirect ? 0 : (size_t)NW * KW * LT * 16 * kPowers) + (x > red ? x : red);
 }
 
+// More than 64 KB of LDS are asked for once for each kernel and device (a bit of `allowed`).
+hipError_t allow_lds(const void *kernel, size_t lds, std::atomic<unsigned long long> &allowed)
+{
+    if (lds <= 64 * 1024) return hipSuccess;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 template <bool kSwiglu, int NW, int KW, int MT, int WT, int D, int KC, int kOcc, bool kDirect, bool kWhole, typename TOut>
 hipError_t launch_whole(const FourGemm &g, int row_tiles, hipStream_t st)
 {
     static_assert(KC || kDirect, "powers by way of LDS are turned over with the chunks");
     const auto kernel = k_four_rows<kSwiglu, NW, KW, MT, WT, D, KC, kOcc, kDirect, kWhole, TOut>;
-    static const hipError_t ready = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds);
-    if (ready != hipSuccess) return ready;
+    const size_t lds = lds_of<kSwiglu, NW, KW, MT, WT, KC, kDirect>(g);
+    static std::atomic<unsigned long long> allowed{0};
+    const hipError_t e = allow_lds((const void *)kernel, lds, allowed);
+    if (e != hipSuccess) return e;
     const int slices = slices_of(g, NW * WT * 16);
     // A slice's row tiles read the same weights and run side by side.  Of sorted rows nobody knows which tiles have none: those workgroups end at once, and
     // come last.  Between the others they upset how these are dealt out to the chip (in turn with eight others 309 us for 163, with 264 169 for 102).
@@ -350,7 +368,7 @@ hipError_t launch_whole(const FourGemm &g, int row_tiles, hipStream_t st)
     const long long units = (all + together - 1) / together * together, most = kMostThreads / (NW * KW * 64) / units;
     // workgroups go on to further row tiles of theirs where a launch could not have one for each
     const int tiles = (int)(most < row_tiles ? most : row_tiles);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(units * tiles)), dim3(NW * KW * 64), (lds_of<kSwiglu, NW, KW, MT, WT, KC, kDirect>(g)), st, g, slices, tiles, together);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(units * tiles)), dim3(NW * KW * 64), lds, st, g, slices, tiles, together);
     return hipGetLastError();
 }
 template <bool kSwiglu, int NW, int KW, int MT, int WT, int D, int KC, int kOcc, bool kDirect, typename TOut>

@@ -48,6 +48,12 @@ def sort_workspace(tokens: int, top_k: int, n_groups: int, device="cuda") -> Opt
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
+def _overwritten(tensors) -> None:
+    """Results that were given count as changed in place: a backward pass that was to read what they held refuses."""
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
+
+
 def _check_routing(ids: torch.Tensor, tokens: int, dev: int):
     if ids.dim() != 2 or ids.shape[0] != tokens:
         raise ValueError(f"ids must be [{tokens}, top_k], is {list(ids.shape)}")
@@ -70,7 +76,7 @@ def _sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev):
         raise ValueError("the workspace must be contiguous and on the device of x")
     if n_groups <= 0:
         raise ValueError(f"n_groups must be positive, is {n_groups}")
-    zero_rest = rows is None
+    zero_rest, written = rows is None, [t for t in (rows, *(order or ())) if t is not None]
     if rows is None or order is None or workspace is None:
         with _owned_by(stream):
             if rows is None:
@@ -87,6 +93,7 @@ def _sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev):
     pk, nk = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     B.moe_sort_tokens(_pack_sort(tokens, top_k, n_groups, n_experts, cols, _DTYPE[dt], zero_rest, pi, pm, px, ld_x, pt, ld_t, po, ps, pr, pk, nk),
                       _current_stream(dev) if stream is None else stream.cuda_stream)
+    _overwritten(written)
     return rows, order
 
 
@@ -97,6 +104,7 @@ def _combine(y, row, weights, out, stream, dev):
         raise ValueError("row must be [tokens, top_k]")
     tokens, top_k = row.shape
     cols, dt = y.shape[1], y.dtype
+    written = [] if out is None else [out]
     if out is None:
         with _owned_by(stream):
             out = torch.empty((tokens, cols), dtype=dt, device=y.device)
@@ -106,6 +114,7 @@ def _combine(y, row, weights, out, stream, dev):
     po, ld_o = _matrix(out, (tokens, cols), dt, dev, "out")
     B.moe_combine_tokens(_pack_combine(tokens, top_k, cols, _DTYPE[dt], py, ld_y, pr, pw, po, ld_o),
                          _current_stream(dev) if stream is None else stream.cuda_stream)
+    _overwritten(written)
     return out
 
 

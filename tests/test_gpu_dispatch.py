@@ -207,6 +207,51 @@ def test_a_gradient_of_a_gradient_is_refused():
         torch.autograd.grad(dx.sum(), x)
 
 
+def test_an_order_that_was_overwritten_has_no_gradient():
+    T, k, S, cols = 8, 2, 4, 64
+    a, b = (routing(s, T, k, S, S, "plain")[0].cuda() for s in (1, 2))
+    x = torch.randn(T, cols, device="cuda")
+    y = torch.randn(T * k, cols, device="cuda", requires_grad=True)
+    rows, order = D().sort_tokens(x, a, S)
+    out = D().combine_tokens(y, order)
+    D().sort_tokens(x, b, S, rows=rows, order=order)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(out.sum(), y)
+
+
+def test_a_captured_step_with_its_backward():
+    """Sort, an expert's product of torch's, combine and all gradients in one graph, on leaves that no eager graph holds."""
+    T, k, S, cols = 40, 4, 8, 128
+    ids = torch.zeros(T, k, dtype=torch.int32, device="cuda")
+    grad = torch.zeros(T, cols, device="cuda")
+    values = [torch.randn(T, cols, device="cuda"), torch.rand(T, k, device="cuda"), torch.randn(T * k, 1, device="cuda")]
+
+    def step(x, w, scale):
+        rows, order = D().sort_tokens(x, ids, S)
+        out = D().combine_tokens(rows * scale, order, w)
+        return (out, *torch.autograd.grad(out, (x, w, scale), grad))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*(v.clone().requires_grad_() for v in values))
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    leaves = [v.clone().requires_grad_() for v in values]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(*leaves)
+    for seed in range(3):
+        ids.copy_(routing(seed, T, k, S + 1, S, "plain")[0])
+        grad.copy_(torch.randn(T, cols))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.detach().clone() for t in captured]
+        want = step(*(v.clone().requires_grad_() for v in values))
+        for a, b in zip(got, want):
+            assert torch.equal(a, b.detach())
+
+
 @pytest.mark.parametrize("T", [64, 1200])
 def test_replays_of_a_graph(T):
     """Sort and combine captured on buffers; every replay is the eager result for what the buffers hold by then."""
