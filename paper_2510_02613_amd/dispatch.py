@@ -15,6 +15,7 @@ Where grad mode is on and x, y or weights require gradients, they are computed b
 """
 from __future__ import annotations
 
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -40,81 +41,87 @@ class Sorted(NamedTuple):
 
 _pack_sort, _pack_combine = B.packer(B.MoESortTokens), B.packer(B.MoECombineTokens)
 _pack_backward = B.packer(B.MoECombineTokensBackward)
+# results that were given count as changed in place: a backward pass that was to read what they held refuses
+_increment_version = torch.autograd.graph.increment_version
+
+
+_workspace_bytes = functools.lru_cache(maxsize=1024)(B.moe_sort_tokens_workspace_bytes)      # of sizes alone
 
 
 def sort_workspace(tokens: int, top_k: int, n_groups: int, device="cuda") -> Optional[torch.Tensor]:
     """A workspace for sort_tokens() of these sizes, or None when it needs none.  One for more tokens is enough for fewer."""
-    n = B.moe_sort_tokens_workspace_bytes(tokens, top_k, n_groups)
+    n = _workspace_bytes(tokens, top_k, n_groups)
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
-def _overwritten(tensors) -> None:
-    """Results that were given count as changed in place: a backward pass that was to read what they held refuses."""
-    if tensors:
-        torch.autograd.graph.increment_version(tensors)
+def _new_order(n_groups, routing, device) -> Order:
+    empty, i32 = torch.empty, torch.int32
+    return Order(empty(n_groups + 1, dtype=i32, device=device), empty(routing[0] * routing[1], dtype=i32, device=device), empty(routing, dtype=i32, device=device))
 
 
-def _check_routing(ids: torch.Tensor, tokens: int, dev: int):
+def _sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev, zero_rest=False):
+    shape, dt = x.shape, x.dtype
+    if len(shape) != 2 or dt not in _DTYPE:
+        raise ValueError("x must be a bfloat16 or float32 matrix")
+    tokens, cols = shape
     if ids.dim() != 2 or ids.shape[0] != tokens:
         raise ValueError(f"ids must be [{tokens}, top_k], is {list(ids.shape)}")
-    return ids.shape[1], _whole(ids, ids.shape, torch.int32, dev, "ids")
-
-
-def _sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev):
-    if x.dim() != 2 or x.dtype not in _DTYPE:
-        raise ValueError("x must be a bfloat16 or float32 matrix")
-    tokens, cols = x.shape
-    top_k, pi = _check_routing(ids, tokens, dev)
-    A, dt = tokens * top_k, x.dtype
+    if n_groups <= 0:
+        raise ValueError(f"n_groups must be positive, is {n_groups}")
+    routing = ids.shape
+    top_k = routing[1]
+    A = tokens * top_k
+    pi = _whole(ids, routing, torch.int32, dev, "ids")
     pm, n_experts = 0, 0
     if expert_map is not None:
         if expert_map.dim() != 1:
             raise ValueError("expert_map must be [n_experts]")
         n_experts = expert_map.shape[0]
-        pm = _whole(expert_map, (n_experts,), torch.int32, dev, "expert_map")
+        pm = _whole(expert_map, expert_map.shape, torch.int32, dev, "expert_map")
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("the workspace must be contiguous and on the device of x")
-    if n_groups <= 0:
-        raise ValueError(f"n_groups must be positive, is {n_groups}")
-    zero_rest, written = rows is None, [t for t in (rows, *(order or ())) if t is not None]
-    if rows is None or order is None or workspace is None:
+    written = [t for t in (rows, *(order or ())) if t is not None]
+    if rows is None or order is None or (workspace is None and _workspace_bytes(tokens, top_k, n_groups)):
         with _owned_by(stream):
             if rows is None:
-                rows = torch.empty((A, cols), dtype=dt, device=x.device)
+                rows, zero_rest = torch.empty((A, cols), dtype=dt, device=x.device), True
             if order is None:
-                order = Order(*(torch.empty(shape, dtype=torch.int32, device=x.device) for shape in ((n_groups + 1,), (A,), (tokens, top_k))))
+                order = _new_order(n_groups, routing, x.device)
             if workspace is None:
                 workspace = sort_workspace(tokens, top_k, n_groups, x.device)
-    po = _whole(order.offsets, (n_groups + 1,), torch.int32, dev, "offsets")
-    ps = _whole(order.source, (A,), torch.int32, dev, "source")
-    pr = _whole(order.row, (tokens, top_k), torch.int32, dev, "row")
-    px, ld_x = _matrix(x, (tokens, cols), dt, dev, "x")
+    offsets, source, row = order
+    po = _whole(offsets, (n_groups + 1,), torch.int32, dev, "offsets")
+    ps = _whole(source, (A,), torch.int32, dev, "source")
+    pr = _whole(row, routing, torch.int32, dev, "row")
+    px, ld_x = _matrix(x, shape, dt, dev, "x")
     pt, ld_t = _matrix(rows, (A, cols), dt, dev, "rows")
     pk, nk = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     B.moe_sort_tokens(_pack_sort(tokens, top_k, n_groups, n_experts, cols, _DTYPE[dt], zero_rest, pi, pm, px, ld_x, pt, ld_t, po, ps, pr, pk, nk),
                       _current_stream(dev) if stream is None else stream.cuda_stream)
-    _overwritten(written)
+    if written:
+        _increment_version(written)
     return rows, order
 
 
 def _combine(y, row, weights, out, stream, dev):
-    if y.dim() != 2 or y.dtype not in _DTYPE:
+    shape, dt, routing = y.shape, y.dtype, row.shape
+    if len(shape) != 2 or dt not in _DTYPE:
         raise ValueError("y must be a bfloat16 or float32 matrix")
-    if row.dim() != 2:
+    if len(routing) != 2:
         raise ValueError("row must be [tokens, top_k]")
-    tokens, top_k = row.shape
-    cols, dt = y.shape[1], y.dtype
-    written = [] if out is None else [out]
-    if out is None:
+    tokens, top_k = routing
+    cols, given = shape[1], out is not None
+    if not given:
         with _owned_by(stream):
             out = torch.empty((tokens, cols), dtype=dt, device=y.device)
-    pr = _whole(row, row.shape, torch.int32, dev, "row")
-    pw = 0 if weights is None else _whole(weights, (tokens, top_k), torch.float32, dev, "weights")
+    pr = _whole(row, routing, torch.int32, dev, "row")
+    pw = 0 if weights is None else _whole(weights, routing, torch.float32, dev, "weights")
     py, ld_y = _matrix(y, (tokens * top_k, cols), dt, dev, "y")
     po, ld_o = _matrix(out, (tokens, cols), dt, dev, "out")
     B.moe_combine_tokens(_pack_combine(tokens, top_k, cols, _DTYPE[dt], py, ld_y, pr, pw, po, ld_o),
                          _current_stream(dev) if stream is None else stream.cuda_stream)
-    _overwritten(written)
+    if given:
+        _increment_version(out)
     return out
 
 
@@ -124,57 +131,73 @@ def _rows16(t: torch.Tensor) -> torch.Tensor:
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
+def _unchanged(t: torch.Tensor, version: int) -> None:
+    if t._version != version:
+        raise RuntimeError("the order of the tokens was overwritten since the call whose gradient is wanted: its buffers were given to another call")
+
+
+def _sort_backward(ctx, grad_rows):
+    if grad_rows is None:
+        return None, None, None, None, None, None
+    row, version = ctx.row
+    _unchanged(row, version)
+    return _combine(_rows16(grad_rows), row, None, None, None, grad_rows.get_device()), None, None, None, None, None
+
+
+def _combine_backward(ctx, grad):
+    if grad is None:
+        return None, None, None, None
+    offsets, row, *versions = ctx.order
+    _unchanged(offsets, versions[0])
+    _unchanged(row, versions[1])
+    y, weights = ctx.saved_tensors
+    grad, dev, dt = _rows16(grad), grad.get_device(), grad.dtype
+    wants_y, wants_w, *_ = ctx.needs_input_grad
+    tokens, top_k = row.shape
+    cols = grad.shape[1]
+    shape = (tokens * top_k, cols)
+    dy = torch.empty(shape, dtype=dt, device=grad.device) if wants_y else None
+    dw = torch.empty(row.shape, dtype=torch.float32, device=grad.device) if wants_w else None
+    py, ld_y = _matrix(y, shape, dt, dev, "y") if wants_w else (0, 0)
+    B.moe_combine_tokens_backward(
+        _pack_backward(tokens, top_k, cols, _DTYPE[dt], grad.data_ptr(), cols, py, ld_y, row.data_ptr(), 0 if weights is None else weights.data_ptr(),
+                       offsets.data_ptr() + 4 * (offsets.shape[0] - 1), dy.data_ptr() if wants_y else 0, cols, dw.data_ptr() if wants_w else 0), _current_stream(dev))
+    return dy, dw, None, None
+
+
+# where a graph of the backward pass is asked for (create_graph), results that refuse a gradient of their own
+_sort_backward_once, _combine_backward_once = once_differentiable(_sort_backward), once_differentiable(_combine_backward)
+
+
 class _SortTokens(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, ids, n_groups, expert_map, workspace):
-        rows, order = _sort(x, ids, n_groups, expert_map, None, None, workspace, None, x.get_device())
-        ctx.save_for_backward(order.row)
-        ctx.mark_non_differentiable(*order)
+    def forward(ctx, x, ids, n_groups, expert_map, order, workspace):
         ctx.set_materialize_grads(False)
-        return rows, order.offsets, order.source, order.row
+        rows = torch.empty((ids.numel(), x.shape[1]), dtype=x.dtype, device=x.device)
+        _sort(x, ids, n_groups, expert_map, rows, order, workspace, None, x.get_device(), zero_rest=True)
+        ctx.row = order.row, order.row._version
+        return rows
 
     @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_rows, *_):
-        if grad_rows is None:
-            return None, None, None, None, None
-        row, = ctx.saved_tensors
-        return _combine(_rows16(grad_rows), row, None, None, None, grad_rows.get_device()), None, None, None, None
+    def backward(ctx, grad_rows):
+        return (_sort_backward_once if torch.is_grad_enabled() else _sort_backward)(ctx, grad_rows)
 
 
 class _CombineTokens(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, weights, offsets, row):
-        ctx.save_for_backward(y if ctx.needs_input_grad[1] else None, weights, offsets, row)
         ctx.set_materialize_grads(False)
+        ctx.save_for_backward(y if ctx.needs_input_grad[1] else None, weights)
+        ctx.order = offsets, row, offsets._version, row._version
         return _combine(y, row, weights, None, None, y.get_device())
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, grad):
-        if grad is None:
-            return None, None, None, None
-        y, weights, offsets, row = ctx.saved_tensors
-        grad, dev, dt = _rows16(grad), grad.get_device(), grad.dtype
-        tokens, top_k = row.shape
-        cols = grad.shape[1]
-        dy = torch.empty((tokens * top_k, cols), dtype=dt, device=grad.device) if ctx.needs_input_grad[0] else None
-        dw = torch.empty((tokens, top_k), dtype=torch.float32, device=grad.device) if ctx.needs_input_grad[1] else None
-        pg, ld_g = _matrix(grad, (tokens, cols), dt, dev, "grad")
-        py, ld_y = (0, 0) if dw is None else _matrix(y, (tokens * top_k, cols), dt, dev, "y")
-        pd, ld_d = (0, 0) if dy is None else _matrix(dy, dy.shape, dt, dev, "grad_y")
-        B.moe_combine_tokens_backward(
-            _pack_backward(tokens, top_k, cols, _DTYPE[dt], pg, ld_g, py, ld_y, row.data_ptr(), 0 if weights is None else weights.data_ptr(),
-                           offsets.data_ptr() + 4 * (offsets.shape[0] - 1), pd, ld_d, 0 if dw is None else dw.data_ptr()), _current_stream(dev))
-        return dy, dw, None, None
+        return (_combine_backward_once if torch.is_grad_enabled() else _combine_backward)(ctx, grad)
 
 
-def _wants_gradient(what, *tensors) -> bool:
-    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in tensors):
-        return False
-    if any(w is not None for w in what):
-        raise ValueError("results that are given and a stream are for calls without a gradient")
-    return True
+def _refuse_given():
+    raise ValueError("results that are given and a stream are for calls without a gradient")
 
 
 def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map: Optional[torch.Tensor] = None,
@@ -186,9 +209,13 @@ def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map
     if dev != _current_device():
         with torch.cuda.device(dev):
             return sort_tokens(x, ids, n_groups, expert_map=expert_map, rows=rows, order=order, workspace=workspace, stream=stream)
-    if _wants_gradient((rows, order, stream), x):
-        got = _SortTokens.apply(x, ids, n_groups, expert_map, workspace)
-        return Sorted(got[0], Order(*got[1:]))
+    if x.requires_grad and torch.is_grad_enabled():
+        if rows is not None or order is not None or stream is not None:
+            _refuse_given()
+        if ids.dim() != 2 or n_groups <= 0 or x.dim() != 2:
+            raise ValueError("x must be [tokens, cols], ids [tokens, top_k] and n_groups positive")
+        order = _new_order(n_groups, ids.shape, x.device)
+        return Sorted(_SortTokens.apply(x, ids, n_groups, expert_map, order, workspace), order)
     return Sorted(*_sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev))
 
 
@@ -199,7 +226,9 @@ def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor
     if dev != _current_device():
         with torch.cuda.device(dev):
             return combine_tokens(y, order, weights, out=out, stream=stream)
-    if _wants_gradient((out, stream), y, weights):
+    if (y.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
+        if out is not None or stream is not None:
+            _refuse_given()
         if order.offsets.dim() != 1 or order.offsets.numel() == 0:
             raise ValueError("offsets must be [n_groups + 1]")
         _whole(order.offsets, order.offsets.shape, torch.int32, dev, "offsets")

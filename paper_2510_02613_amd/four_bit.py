@@ -33,15 +33,13 @@ _pack_quantize, _pack_matmul = B.packer(B.MoEFourBitQuantize), B.packer(B.MoEFou
 _pack_swiglu = B.packer(B.MoEFourBitSwiglu)
 
 
-def _one_of(t: torch.Tensor, dtypes, what: str):
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, is {t.dtype}")
-    return t.dtype
+def _named(t: torch.Tensor, dtypes):
+    """t's type where it is one that names such bytes, else the plain one, for the check that refuses it."""
+    return t.dtype if t.dtype in dtypes else torch.uint8
 
 
-def _no_gradient(*tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
+def _refuse_gradient():
+    raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
 
 
 def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None,
@@ -51,7 +49,8 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
     if dev != _current_device():      # kernels run on the tensors' device, whichever is current
         with torch.cuda.device(dev):
             return quantize(x, q=q, scale=scale, values=values, stream=stream)
-    _no_gradient(x, values)
+    if torch.is_grad_enabled() and (x.requires_grad or (values is not None and values.requires_grad)):
+        _refuse_gradient()
     if x.dim() != 2 or x.dtype not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
     rows, cols = x.shape
@@ -60,47 +59,34 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
             q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device) if q is None else q
             scale = torch.empty((rows, cols // GROUP), dtype=torch.uint8, device=x.device) if scale is None else scale
     px, ld_x = _matrix(x, (rows, cols), x.dtype, dev, "x")
-    pq, ld_q = _matrix(q, (rows, cols // 2), _one_of(q, _CODES, "q"), dev, "q")
-    ps, ld_s = _matrix(scale, (rows, cols // GROUP), _one_of(scale, _POWERS, "scale"), dev, "scale")
+    pq, ld_q = _matrix(q, (rows, cols // 2), _named(q, _CODES), dev, "q")
+    ps, ld_s = _matrix(scale, (rows, cols // GROUP), _named(scale, _POWERS), dev, "scale")
     pv, ld_v = (0, 0) if values is None else _matrix(values, (rows, cols), x.dtype, dev, "values")
     B.moe_four_bit_quantize(_pack_quantize(rows, cols, _DTYPE[x.dtype], px, ld_x, pq, ld_q, ps, ld_s, pv, ld_v),
                             _current_stream(dev) if stream is None else stream.cuda_stream)
     return FourBit(q, scale)
 
 
-def _product(a, w, w_scale, offsets, add, out, out_dtype, stream, dev, swiglu):
-    """Checks both products' arguments; (m, result columns, k, groups, dtype, addresses and strides, out)."""
-    _no_gradient(a, add, out)
-    if a.dim() != 2:
-        raise ValueError("a must be a matrix")
-    m, k = a.shape
+def _weights(w, w_scale, offsets, k, dev):
+    """Checks the weights; (groups, weight rows of a group, addresses of offsets, w and w_scale)."""
     if offsets is None:
         if w.dim() != 2:
             raise ValueError("w must be [n, k / 2] without offsets")
-        groups, n = 1, w.shape[0]
-        po, lead = 0, (n,)
+        n, = lead = w.shape[:1]
+        groups, po = 1, 0
     else:
         if w.dim() != 3:
             raise ValueError("w must be [groups, n, k / 2] with offsets")
-        groups, n = w.shape[0], w.shape[1]
-        po, lead = _whole(offsets, (groups + 1,), torch.int32, dev, "offsets"), (groups, n)
-    cols = n // 2 if swiglu else n
-    if swiglu and n % 2:
-        raise ValueError("w must hold as many gate rows as up rows")
-    if out is None:
-        # rows of the result start on 16 bytes whatever n is; those in no group are zeros
-        with _owned_by(stream):
-            make = torch.empty if offsets is None else torch.zeros
-            out = make((m, (cols + 7) // 8 * 8), dtype=add.dtype if add is not None else out_dtype, device=a.device)[:, :cols]
-    dt = out.dtype
-    if dt not in _DTYPE:
-        raise ValueError("out must be bfloat16 or float32")
-    pa, ld_a = _matrix(a, (m, k), torch.bfloat16, dev, "a")
-    pw = _whole(w, lead + (k // 2,), _one_of(w, _CODES, "w"), dev, "w")
-    ps = _whole(w_scale, lead + (k // GROUP,), _one_of(w_scale, _POWERS, "w_scale"), dev, "w_scale")
-    pd, ld_d = (0, 0) if add is None else _matrix(add, (m, cols), dt, dev, "add")
-    pt, ld_t = _matrix(out, (m, cols), dt, dev, "out")
-    return m, cols, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t, out
+        groups, n = lead = w.shape[:2]
+        po = _whole(offsets, (groups + 1,), torch.int32, dev, "offsets")
+    return (groups, n, po, _whole(w, (*lead, k // 2), _named(w, _CODES), dev, "w"),
+            _whole(w_scale, (*lead, k // GROUP), _named(w_scale, _POWERS), dev, "w_scale"))
+
+
+def _result(m, cols, dtype, device, offsets, stream):
+    """Rows of the result start on 16 bytes whatever their width; those in no group are zeros."""
+    with _owned_by(stream):
+        return (torch.empty if offsets is None else torch.zeros)((m, (cols + 7) // 8 * 8), dtype=dtype, device=device)[:, :cols]
 
 
 def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
@@ -111,8 +97,19 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return matmul(a, w, w_scale, offsets=offsets, add=add, out=out, out_dtype=out_dtype, stream=stream)
-    m, n, k, groups, dt, pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t, out = _product(a, w, w_scale, offsets, add, out, out_dtype, stream, dev, False)
-    B.moe_four_bit_matmul(_pack_matmul(m, n, k, groups, dt, pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t),
+    if torch.is_grad_enabled() and (a.requires_grad or (add is not None and add.requires_grad) or (out is not None and out.requires_grad)):
+        _refuse_gradient()
+    m, k = a.shape
+    groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
+    if out is None:
+        out = _result(m, n, out_dtype if add is None else add.dtype, a.device, offsets, stream)
+    dt = out.dtype
+    if dt not in _DTYPE:
+        raise ValueError("out must be bfloat16 or float32")
+    pa, ld_a = _matrix(a, (m, k), torch.bfloat16, dev, "a")
+    pd, ld_d = (0, 0) if add is None else _matrix(add, (m, n), dt, dev, "add")
+    pt, ld_t = _matrix(out, (m, n), dt, dev, "out")
+    B.moe_four_bit_matmul(_pack_matmul(m, n, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
     return out
 
@@ -124,7 +121,20 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return swiglu(a, w, w_scale, offsets=offsets, out=out, out_dtype=out_dtype, stream=stream)
-    m, inter, k, groups, dt, pa, ld_a, po, pw, ps, _, _, pt, ld_t, out = _product(a, w, w_scale, offsets, None, out, out_dtype, stream, dev, True)
-    B.moe_four_bit_swiglu(_pack_swiglu(m, inter, k, groups, dt, pa, ld_a, po, pw, ps, pt, ld_t),
+    if torch.is_grad_enabled() and (a.requires_grad or (out is not None and out.requires_grad)):
+        _refuse_gradient()
+    m, k = a.shape
+    groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
+    if n % 2:
+        raise ValueError("w must hold as many gate rows as up rows")
+    inter = n // 2
+    if out is None:
+        out = _result(m, inter, out_dtype, a.device, offsets, stream)
+    dt = out.dtype
+    if dt not in _DTYPE:
+        raise ValueError("out must be bfloat16 or float32")
+    pa, ld_a = _matrix(a, (m, k), torch.bfloat16, dev, "a")
+    pt, ld_t = _matrix(out, (m, inter), dt, dev, "out")
+    B.moe_four_bit_swiglu(_pack_swiglu(m, inter, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
     return out
