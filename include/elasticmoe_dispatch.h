@@ -27,7 +27,7 @@ extern "C" {
  */
 
 /*
- * rows[r] = x[source[r] / top_k]: the tokens' rows in the order of their groups.  x and rows may both be NULL: only the order is wanted.
+ * rows[r] = x[source[r] / top_k]: the tokens' rows in the order of their groups.
  * Rows behind the last one are not touched, or zeroed where zero_rest is set.  No tokens: offsets are zeros.
  * Many assignments are counted first, in the caller's workspace of moe_sort_tokens_workspace_bytes (0: none needed; more assignments or groups of
  * the same kind never need less).  Calls that share a workspace must be ordered against each other (one stream).
@@ -41,9 +41,9 @@ typedef struct {
     int32_t zero_rest;
     const int32_t *ids;           /* [tokens, top_k] */
     const int32_t *expert_map;    /* [n_experts] or NULL */
-    const void *x;                /* [tokens, cols] or NULL */
+    const void *x;                /* [tokens, cols] */
     int64_t ld_x;
-    void   *rows;                 /* [tokens * top_k, cols], NULL iff x is */
+    void   *rows;                 /* [tokens * top_k, cols] */
     int64_t ld_rows;
     int32_t *offsets;             /* [n_groups + 1] */
     int32_t *source;              /* [tokens * top_k] */

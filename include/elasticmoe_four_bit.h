@@ -40,7 +40,7 @@ moe_status_t moe_four_bit_quantize(const moe_four_bit_quantize_t *args, void *hi
 
 /*
  * out = a w^T (+ add): bf16 rows times 4-bit weights.  With offsets (device, as moe_sort_tokens writes them) row r of group g, offsets[g] <= r <
- * offsets[g + 1], takes the weights w[g]; rows in no group are not touched, and what offsets name outside [0, m) is left out.
+ * offsets[g + 1], takes the weights w[g]; rows in no group are not touched, and what offsets name outside [0, m) is left out.  Offsets must not decrease.
  * A weight times its power of two is a bf16 number, so that products are exact; their sums are fp32's, rounded once at the end.  The order of a sum
  * depends on the sizes of the call, not on what runs beside it.  out may be add itself (same address and ld).
  * Made for few rows a group, where the weights' bytes are what a product costs; many rows are right too, at some times the time a bf16 product would take.

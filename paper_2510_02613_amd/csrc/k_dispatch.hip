@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(SortJob s, int per, int
     int32_t *first = lds, *front = lds + bins;
     const int block = a0 / kSortBlock;
     constexpr int U = 4;                  // runs of a batch, at most
-    const int runs = (s.chunks + 63) / 64, batches = (runs + batch - 1) / batch, items = s.x ? nt * batches : 0;
+    const int runs = (s.chunks + 63) / 64, batches = (runs + batch - 1) / batch, items = nt * batches;
     u32x4 v[U];
     auto load = [&](int i) __attribute__((always_inline)) {
         const int t = i / batches, run = (i - t * batches) * batch;
@@ -212,7 +212,6 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(SortJob s, int per, int
             dest[lane] = here ? r : (s.zero_rest ? ~r : (int)0x80000000);    // negative: not a row; ~r: zeros go there
         }
     }
-    if (!s.x) return;
     __syncthreads();
     for (int i = i0; i < items; i += stride) {
         const int t = i / batches, run = (i - t * batches) * batch;
@@ -360,7 +359,7 @@ hipError_t launch_sort_tokens(const SortJob &j, hipStream_t st)
 {
     const int bins = j.n_groups + 1, n_blocks = sort_blocks(j.tokens, j.top_k);
     int per = 64 / j.top_k;
-    const int runs = j.x ? (j.chunks + 63) / 64 : 1;
+    const int runs = (j.chunks + 63) / 64;
     // few tokens: fewer of them to a workgroup, then shorter batches on more workgroups
     while (per > 1 && (j.tokens + per - 1) / per < 512) per = (per + 1) / 2;
     const int gx = j.tokens > 0 ? (j.tokens + per - 1) / per : 1;
@@ -369,7 +368,7 @@ hipError_t launch_sort_tokens(const SortJob &j, hipStream_t st)
     const int batches = (runs + batch - 1) / batch;
     int gy = 1;
     while (gy * kWaves < batches * per && gx * gy < 512) gy *= 2;
-    const dim3 grid(gx, j.x ? gy : 1);
+    const dim3 grid(gx, gy);
     const size_t lds = 2 * bins * sizeof(int32_t);
     if (n_blocks == 0) {
         hipLaunchKernelGGL(k_sort_place<kCountAll>, grid, dim3(kThreads), lds, st, j, per, batch, 0);

@@ -72,16 +72,13 @@ moe_status_t moe_sort_tokens(const moe_sort_tokens_t *n, void *hip_stream)
         if (n->n_experts <= 0) return fail(MOE_ERR_SHAPE, "n_experts %d must be positive with an expert_map", n->n_experts);
         EMOE_TRY(check_words(n->expert_map, "expert_map"));
     }
-    if ((n->x != nullptr) != (n->rows != nullptr)) return fail(MOE_ERR_ARG, "x and rows must be given together");
     SortJob j = {};
     if (n->tokens > 0) {
         EMOE_TRY(check_words(n->ids, "ids"));
         EMOE_TRY(check_words(n->source, "source"));
         EMOE_TRY(check_words(n->row, "row"));
-        if (n->x) {
-            EMOE_TRY(check_rows(n->x, n->ld_x, n->cols, n->dtype, "x"));
-            EMOE_TRY(check_rows(n->rows, n->ld_rows, n->cols, n->dtype, "rows"));
-        }
+        EMOE_TRY(check_rows(n->x, n->ld_x, n->cols, n->dtype, "x"));
+        EMOE_TRY(check_rows(n->rows, n->ld_rows, n->cols, n->dtype, "rows"));
         const size_t need = moe_sort_tokens_workspace_bytes(n->tokens, n->top_k, n->n_groups);
         if (need) {
             if (!n->workspace || !aligned(n->workspace, 16)) return fail(MOE_ERR_ARG, "a 16-byte aligned workspace is needed");

@@ -229,8 +229,8 @@ def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor
     if (y.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
         if out is not None or stream is not None:
             _refuse_given()
-        if order.offsets.dim() != 1 or order.offsets.numel() == 0:
-            raise ValueError("offsets must be [n_groups + 1]")
+        if order.offsets is None or order.offsets.dim() != 1 or order.offsets.numel() == 0:
+            raise ValueError("a gradient wants the order's offsets, [n_groups + 1]")
         _whole(order.offsets, order.offsets.shape, torch.int32, dev, "offsets")
         return _CombineTokens.apply(y, weights, order.offsets, order.row)
     return _combine(y, order.row, weights, out, stream, dev)

@@ -153,6 +153,36 @@ def test_gradient_of_sort(T, k, E, S, cols, dt, kind):
     R.check(dx, want, off, "dx")
 
 
+def test_backward_leaves_the_rest_alone_without_its_number():
+    """The call itself: rows of grad_y behind the last are touched only where the number of rows is given; either result alone."""
+    from paper_2510_02613_amd import binding as B
+    T, k, E, S, cols, dt = 33, 6, 64, 20, 520, BF16
+    ids, m, row, y, w = made(T, k, E, S, cols, dt, "map")
+    offsets, _, _ = R.order(ids, S, m)
+    total = int(offsets[-1])
+    g = torch.randn(T, cols, generator=torch.Generator().manual_seed(9)).to(dt)
+    dy, off_y, dw, off_w = R.backward(g, y, row, w)
+    dev = [t.cuda() for t in (g, y, row, w, offsets)]
+    for n_rows in (0, dev[4].data_ptr() + 4 * S):
+        for wants in ((True, True), (True, False), (False, True)):
+            gy = padded(torch.full((T * k, cols), 7.0, dtype=dt, device="cuda"), 3.0)
+            gw = torch.full((T, k), 7.0, device="cuda")
+            B.moe_combine_tokens_backward(B.MoECombineTokensBackward(
+                tokens=T, top_k=k, cols=cols, dtype=B.MOE_BF16, grad_out=dev[0].data_ptr(), ld_grad_out=cols, y=dev[1].data_ptr(), ld_y=cols, row=dev[2].data_ptr(),
+                weights=dev[3].data_ptr(), n_rows=n_rows, grad_y=gy.data_ptr() if wants[0] else 0, ld_grad_y=gy.stride(0), grad_weights=gw.data_ptr() if wants[1] else 0),
+                torch.cuda.current_stream().cuda_stream)
+            torch.cuda.synchronize()
+            if wants[0]:
+                R.check(gy[:total], dy[:total], off_y[:total], "grad_y")
+                assert gy[total:].eq(0.0 if n_rows else 7.0).all() and gy.as_strided((T * k, 16), gy.stride(), cols).eq(3.0).all()
+            else:
+                assert gy.eq(7.0).all()
+            if wants[1]:
+                R.check(gw, dw, off_w, "grad_weights")
+            else:
+                assert gw.eq(7.0).all()
+
+
 def test_gradients_by_differences():
     """Sorting and adding up again is linear in x and in the weights: its differences along a direction are the gradient's products with it."""
     T, k, E, S, cols = 37, 4, 16, 11, 96

@@ -132,6 +132,38 @@ def test_grouped_products_of_whole_numbers(counts, groups, n, k, out):
     assert given.as_strided((m, 16), given.stride(), n).eq(3.0).all()
 
 
+# Every form of the kernel, k in whole lines of 256 columns and not: which one runs goes by the workgroups it would have
+FORMS = [(2100, 1600, 512), (2100, 1600, 288), (1300, 1100, 512), (1300, 1100, 352), (1300, 1100, 1280), (1300, 1100, 1120), (160, 1800, 512), (160, 1800, 544), (100, 2056, 800),
+         (16, 100, 2816), (16, 100, 2848), (40, 33, 7168), (1, 64, 8192)]
+
+
+@pytest.mark.parametrize("m,n,k", FORMS)
+def test_every_form_of_the_product(m, n, k):
+    g = torch.Generator().manual_seed(m + n + k)
+    (q, s), a = whole_weights(g, n, k), whole_rows(g, m, k)
+    want = a.double() @ R.values(q, s).t()
+    for out in (BF16, F32):
+        assert torch.equal(Q().matmul(a.cuda(), q.cuda(), s.cuda(), out_dtype=out).cpu(), want.float().to(out))
+
+
+GROUP_FORMS = [([3] * 40, 2048, 768), ([3] * 40, 2048, 544), ([2, 3, 4, 0] * 10, 2048, 1312), ([3] * 40, 2048, 1536), ([20, 40, 0, 17] * 10, 1024, 512), ([20, 40, 0, 17] * 10, 1024, 1120),
+               ([1] + [0] * 70 + [5] + [0] * 200, 48, 160), ([0] * 500 + [2] + [0] * 300 + [1] + [0] * 99, 272, 96), ([0] * 1999 + [40], 16, 32), ([200] * 3 + [0] * 4 + [1000], 520, 96)]
+
+
+@pytest.mark.parametrize("counts,n,k", GROUP_FORMS)
+def test_every_form_of_the_grouped_product(counts, n, k):
+    g = torch.Generator().manual_seed(n + k)
+    groups, total = len(counts), sum(counts)
+    (q, s), a = whole_weights(g, groups, n, k), whole_rows(g, total + 3, k)
+    off = offsets_of(counts)
+    got = Q().matmul(a.cuda(), q.cuda(), s.cuda(), offsets=off.cuda(), out_dtype=F32).cpu()
+    assert not got[total:].any()
+    for e in range(groups):
+        lo, hi = off[e], off[e + 1]
+        if hi > lo:
+            assert torch.equal(got[lo:hi].double(), a[lo:hi].double() @ R.values(q[e], s[e]).t()), e
+
+
 def test_offsets_that_leave_the_rows_are_cut():
     g = torch.Generator().manual_seed(3)
     (q, s), a = whole_weights(g, 4, 32, 64), whole_rows(g, 10, 64)
@@ -204,6 +236,33 @@ def test_swiglu(m, inter, k, out):
     given = padded(torch.full((m + 2, inter), 7.0, dtype=out, device="cuda"), 3.0)
     Q().swiglu(padded(a.cuda()), q.cuda(), s.cuda(), out=given[:m])
     assert torch.equal(given[:m], got) and given[m:].eq(7.0).all() and given.as_strided((m + 2, 16), given.stride(), inter).eq(3.0).all()
+
+
+@pytest.mark.parametrize("m,inter,k", [(1300, 1100, 64), (1300, 1100, 288), (2500, 500, 4128), (200, 800, 512), (200, 800, 544), (200, 520, 1024), (200, 520, 1056), (16, 100, 7168), (17, 33, 4128),
+                                       (300, 2100, 4352)])
+def test_every_form_of_swiglu(m, inter, k):
+    a, q, s = case(m + k, m, inter, k)
+    rows = torch.randperm(m, generator=torch.Generator().manual_seed(1))[:64]
+    want, off = R.swiglu(a[rows].double(), torch.zeros(len(rows), k).double(), R.values(q, s))
+    for out in (BF16, F32):
+        got = Q().swiglu(a.cuda(), q.cuda(), s.cuda(), out_dtype=out)[rows.cuda()]
+        R.check(got, want, off)
+        R.check_norm(got, want, out)
+
+
+@pytest.mark.parametrize("counts,inter,k", [([20, 40, 0, 17] * 10, 512, 544), ([20, 40, 0, 17] * 10, 512, 512), ([3] * 40, 1024, 4352), ([3] * 40, 1024, 4128), ([20, 40, 0, 17] * 5, 2048, 4128),
+                                            ([3] * 20, 640, 2048), ([0] * 500 + [2] + [0] * 399, 48, 96), ([1, 0, 0, 0] * 8, 2048, 4352)])
+def test_every_form_of_grouped_swiglu(counts, inter, k):
+    groups, total = len(counts), sum(counts)
+    a, q, s = case(k, total + 3, inter, k, groups)
+    off = offsets_of(counts)
+    got = Q().swiglu(a.cuda(), q.cuda(), s.cuda(), offsets=off.cuda(), out_dtype=F32)
+    assert not got[total:].any()
+    for e in [e for e in range(groups) if counts[e]][::max(1, groups // 5)]:
+        lo, hi = off[e], off[e + 1]
+        want, far = R.swiglu(a[lo:hi].double(), torch.zeros(hi - lo, k).double(), R.values(q[e], s[e]))
+        R.check(got[lo:hi], want, far)
+        R.check_norm(got[lo:hi], want, F32)
 
 
 @pytest.mark.parametrize("counts,groups,n,k", GROUPED)
