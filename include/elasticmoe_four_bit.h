@@ -43,7 +43,7 @@ moe_status_t moe_four_bit_quantize(const moe_four_bit_quantize_t *args, void *hi
  * offsets[g + 1], takes the weights w[g]; rows in no group are not touched, and what offsets name outside [0, m) is left out.  Offsets must not decrease.
  * A weight times its power of two is a bf16 number, so that products are exact; their sums are fp32's, rounded once at the end.  The order of a sum
  * depends on the sizes of the call, not on what runs beside it.  out may be add itself (same address and ld).
- * Made for few rows a group, where the weights' bytes are what a product costs; many rows are right too, at some times the time a bf16 product would take.
+ * Made for few rows a group, where the weights' bytes are what a product costs; many rows work too, at about half the rate of a bf16 product.
  *   MOE_ERR_UNSUPPORTED: k no multiple of 32; m, n or k > 2^21; ld_a >= 2^24; groups > 2047; more tiles than a launch can have workgroups.
  */
 typedef struct {
