@@ -75,7 +75,8 @@ moe_status_t moe_combine_tokens(const moe_combine_tokens_t *args, void *hip_stre
  * The gradient of the above, for grad_out = the gradient of out:
  *     grad_y[row[t, j]] = weights[t, j] * grad_out[t],   grad_weights[t, j] = <grad_out[t], y[row[t, j]]>, 0 where there is no row,
  * each rounded once from fp32; either may be NULL, not both.  Entries of row must differ from each other, as those of moe_sort_tokens do.
- * Rows of grad_y behind the last one are not touched, or zeroed where n_rows is given.
+ * Rows of grad_y that no entry of row names -- those behind the last one, those of assignments whose entry a caller set to -1 -- are not touched, or
+ * zeroed where source is given.
  */
 typedef struct {
     int32_t tokens, top_k, cols;
@@ -86,7 +87,7 @@ typedef struct {
     int64_t ld_y;
     const int32_t *row;           /* [tokens, top_k] */
     const float *weights;         /* [tokens, top_k] or NULL: ones */
-    const int32_t *n_rows;        /* NULL, or where the number of rows stands (offsets + n_groups) */
+    const int32_t *source;        /* [tokens * top_k] as moe_sort_tokens writes it, or NULL */
     void   *grad_y;               /* [tokens * top_k, cols] or NULL */
     int64_t ld_grad_y;
     float  *grad_weights;         /* [tokens, top_k] or NULL */

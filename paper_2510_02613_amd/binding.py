@@ -111,7 +111,7 @@ class MoECombineTokens(ctypes.Structure):
 class MoECombineTokensBackward(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int32), ("top_k", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("grad_out", ctypes.c_void_p), ("ld_grad_out", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
-                ("row", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("n_rows", ctypes.c_void_p),
+                ("row", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("source", ctypes.c_void_p),
                 ("grad_y", ctypes.c_void_p), ("ld_grad_y", ctypes.c_int64), ("grad_weights", ctypes.c_void_p)]
 
 

@@ -26,7 +26,7 @@ struct CombineJob {
     const char *y, *grad_out;             // backward: both
     char *out, *grad_y;
     int64_t ld_y, ld_out, ld_grad_out, ld_grad_y;
-    const int32_t *row, *n_rows;
+    const int32_t *row, *source;
     const float *weights;
     float *grad_weights;
 };

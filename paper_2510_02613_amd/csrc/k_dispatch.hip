@@ -304,8 +304,11 @@ __global__ __launch_bounds__(kThreads) void k_combine_rows_backward(CombineJob p
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int A = p.tokens * p.top_k;
     for (int64_t a = (int64_t)blockIdx.x * kWaves + wave; a < A; a += (int64_t)gridDim.x * kWaves) {
-        if (p.grad_y && p.n_rows && a >= *p.n_rows)
-            for (int c = lane; c < p.chunks; c += 64) *(u32x4 *)(p.grad_y + a * p.ld_grad_y + (int64_t)c * 16) = (u32x4){0, 0, 0, 0};
+        if (p.grad_y && p.source) {       // row a, if it is nobody's
+            const int of = p.source[a];
+            if ((unsigned)of >= (unsigned)A || p.row[of] != (int)a)
+                for (int c = lane; c < p.chunks; c += 64) *(u32x4 *)(p.grad_y + a * p.ld_grad_y + (int64_t)c * 16) = (u32x4){0, 0, 0, 0};
+        }
         const int r = p.row[a];
         if ((unsigned)r >= (unsigned)A) {
             if (p.grad_weights && lane == 0) p.grad_weights[a] = 0.f;

@@ -131,8 +131,8 @@ moe_status_t moe_combine_tokens_backward(const moe_combine_tokens_backward_t *n,
     CombineJob j = {};
     if (n->grad_y) {
         EMOE_TRY(check_rows(n->grad_y, n->ld_grad_y, n->cols, n->dtype, "grad_y"));
-        if (n->n_rows) EMOE_TRY(check_words(n->n_rows, "n_rows"));
-        j.grad_y = (char *)n->grad_y; j.ld_grad_y = n->ld_grad_y * es; j.n_rows = n->n_rows;
+        if (n->source) EMOE_TRY(check_words(n->source, "source"));
+        j.grad_y = (char *)n->grad_y; j.ld_grad_y = n->ld_grad_y * es; j.source = n->source;
     }
     if (n->grad_weights) {
         EMOE_TRY(check_words(n->grad_weights, "grad_weights"));

@@ -147,8 +147,8 @@ def _sort_backward(ctx, grad_rows):
 def _combine_backward(ctx, grad):
     if grad is None:
         return None, None, None, None
-    offsets, row, *versions = ctx.order
-    _unchanged(offsets, versions[0])
+    source, row, *versions = ctx.order
+    _unchanged(source, versions[0])
     _unchanged(row, versions[1])
     y, weights = ctx.saved_tensors
     grad, dev, dt = _rows16(grad), grad.get_device(), grad.dtype
@@ -161,7 +161,7 @@ def _combine_backward(ctx, grad):
     py, ld_y = _matrix(y, shape, dt, dev, "y") if wants_w else (0, 0)
     B.moe_combine_tokens_backward(
         _pack_backward(tokens, top_k, cols, _DTYPE[dt], grad.data_ptr(), cols, py, ld_y, row.data_ptr(), 0 if weights is None else weights.data_ptr(),
-                       offsets.data_ptr() + 4 * (offsets.shape[0] - 1), dy.data_ptr() if wants_y else 0, cols, dw.data_ptr() if wants_w else 0), _current_stream(dev))
+                       source.data_ptr(), dy.data_ptr() if wants_y else 0, cols, dw.data_ptr() if wants_w else 0), _current_stream(dev))
     return dy, dw, None, None
 
 
@@ -185,10 +185,10 @@ class _SortTokens(torch.autograd.Function):
 
 class _CombineTokens(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, y, weights, offsets, row):
+    def forward(ctx, y, weights, source, row):
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(y if ctx.needs_input_grad[1] else None, weights)
-        ctx.order = offsets, row, offsets._version, row._version
+        ctx.order = source, row, source._version, row._version
         return _combine(y, row, weights, None, None, y.get_device())
 
     @staticmethod
@@ -198,6 +198,11 @@ class _CombineTokens(torch.autograd.Function):
 
 def _refuse_given():
     raise ValueError("results that are given and a stream are for calls without a gradient")
+
+
+def _refuse_leaf(given):
+    if given.requires_grad and torch.is_grad_enabled():
+        raise ValueError("results that are given must not require a gradient")
 
 
 def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map: Optional[torch.Tensor] = None,
@@ -216,12 +221,15 @@ def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map
             raise ValueError("x must be [tokens, cols], ids [tokens, top_k] and n_groups positive")
         order = _new_order(n_groups, ids.shape, x.device)
         return Sorted(_SortTokens.apply(x, ids, n_groups, expert_map, order, workspace), order)
+    if rows is not None:
+        _refuse_leaf(rows)
     return Sorted(*_sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev))
 
 
 def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """out[t] = sum over j of weights[t, j] * y[order.row[t, j]], of the assignments that have a row; weights float32 [tokens, top_k], None: ones."""
+    """out[t] = sum over j of weights[t, j] * y[order.row[t, j]], of the assignments that have a row; weights float32 [tokens, top_k], None: ones.
+    Entries of order.row may be set to -1 (assignments that are dropped); rows that none names have a gradient of zeros."""
     dev = _device_of(y)
     if dev != _current_device():
         with torch.cuda.device(dev):
@@ -229,8 +237,10 @@ def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor
     if (y.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
         if out is not None or stream is not None:
             _refuse_given()
-        if order.offsets is None or order.offsets.dim() != 1 or order.offsets.numel() == 0:
-            raise ValueError("a gradient wants the order's offsets, [n_groups + 1]")
-        _whole(order.offsets, order.offsets.shape, torch.int32, dev, "offsets")
-        return _CombineTokens.apply(y, weights, order.offsets, order.row)
+        if order.source is None:
+            raise ValueError("a gradient wants the order's source, [tokens * top_k]")
+        _whole(order.source, (order.row.numel(),), torch.int32, dev, "source")
+        return _CombineTokens.apply(y, weights, order.source, order.row)
+    if out is not None:
+        _refuse_leaf(out)
     return _combine(y, order.row, weights, out, stream, dev)

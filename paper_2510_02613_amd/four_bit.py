@@ -38,6 +38,10 @@ def _named(t: torch.Tensor, dtypes):
     return t.dtype if t.dtype in dtypes else torch.uint8
 
 
+# results that were given count as changed in place
+_increment_version = torch.autograd.graph.increment_version
+
+
 def _refuse_gradient():
     raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
 
@@ -54,6 +58,7 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
     if x.dim() != 2 or x.dtype not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
     rows, cols = x.shape
+    written = [t for t in (q, scale, values) if t is not None]
     if q is None or scale is None:
         with _owned_by(stream):
             q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device) if q is None else q
@@ -64,6 +69,8 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
     pv, ld_v = (0, 0) if values is None else _matrix(values, (rows, cols), x.dtype, dev, "values")
     B.moe_four_bit_quantize(_pack_quantize(rows, cols, _DTYPE[x.dtype], px, ld_x, pq, ld_q, ps, ld_s, pv, ld_v),
                             _current_stream(dev) if stream is None else stream.cuda_stream)
+    if written:
+        _increment_version(written)
     return FourBit(q, scale)
 
 
@@ -101,7 +108,8 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
         _refuse_gradient()
     m, k = a.shape
     groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _result(m, n, out_dtype if add is None else add.dtype, a.device, offsets, stream)
     dt = out.dtype
     if dt not in _DTYPE:
@@ -111,6 +119,8 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     pt, ld_t = _matrix(out, (m, n), dt, dev, "out")
     B.moe_four_bit_matmul(_pack_matmul(m, n, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
+    if given:
+        _increment_version(out)
     return out
 
 
@@ -128,7 +138,8 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if n % 2:
         raise ValueError("w must hold as many gate rows as up rows")
     inter = n // 2
-    if out is None:
+    given = out is not None
+    if not given:
         out = _result(m, inter, out_dtype, a.device, offsets, stream)
     dt = out.dtype
     if dt not in _DTYPE:
@@ -137,4 +148,6 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     pt, ld_t = _matrix(out, (m, inter), dt, dev, "out")
     B.moe_four_bit_swiglu(_pack_swiglu(m, inter, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
+    if given:
+        _increment_version(out)
     return out

@@ -49,7 +49,7 @@ def combine(**kw):
 
 
 def backward(**kw):
-    d = dict(tokens=4, top_k=8, cols=256, dtype=B.MOE_BF16, grad_out=0x10000, ld_grad_out=256, y=0x20000, ld_y=256, row=0x30000, weights=0x40000, n_rows=0x50000,
+    d = dict(tokens=4, top_k=8, cols=256, dtype=B.MOE_BF16, grad_out=0x10000, ld_grad_out=256, y=0x20000, ld_y=256, row=0x30000, weights=0x40000, source=0x50000,
              grad_y=0x60000, ld_grad_y=256, grad_weights=0x70000)
     d.update(kw)
     return lambda: B.moe_combine_tokens_backward(B.MoECombineTokensBackward(**d))
@@ -82,7 +82,7 @@ def test_combine_refuses(kw, status):
 
 @pytest.mark.parametrize("kw,status", COMMON + [
     (dict(grad_out=0), ARG), (dict(grad_out=0x10004), ARG), (dict(ld_grad_out=8), ARG), (dict(y=0), ARG), (dict(y=0x20008), ARG), (dict(ld_y=255), ARG), (dict(weights=0x40002), ARG),
-    (dict(n_rows=0x50001), ARG), (dict(grad_y=0x60008), ARG), (dict(ld_grad_y=8), ARG), (dict(grad_weights=0x70002), ARG), (dict(grad_y=0, grad_weights=0), ARG)])
+    (dict(source=0x50001), ARG), (dict(grad_y=0x60008), ARG), (dict(ld_grad_y=8), ARG), (dict(grad_weights=0x70002), ARG), (dict(grad_y=0, grad_weights=0), ARG)])
 def test_backward_refuses(kw, status):
     refused(backward(**kw), status)
 
@@ -127,7 +127,11 @@ def test_the_python_calls_refuse(monkeypatch):
     leaf = torch.zeros(4, 64, requires_grad=True)
     bad += [lambda: D.sort_tokens(leaf, ids, 3, rows=torch.zeros(8, 64)), lambda: D.sort_tokens(leaf, ids, 3, order=order), lambda: D.sort_tokens(leaf, ids, 3, stream=object()),
             lambda: D.combine_tokens(torch.zeros(8, 64, requires_grad=True), order, out=torch.zeros(4, 64)),
-            lambda: D.combine_tokens(torch.zeros(8, 64, requires_grad=True), order._replace(offsets=order.offsets.long()))]
+            lambda: D.combine_tokens(torch.zeros(8, 64, requires_grad=True), order._replace(source=order.source.long())),
+            lambda: D.combine_tokens(torch.zeros(8, 64, requires_grad=True), order._replace(source=order.source[:7])),
+            lambda: D.combine_tokens(torch.zeros(8, 64, requires_grad=True), order._replace(source=None)),
+            lambda: D.sort_tokens(x, ids, 3, rows=torch.zeros(8, 64, requires_grad=True)),
+            lambda: D.combine_tokens(torch.zeros(8, 64), order, out=torch.zeros(4, 64, requires_grad=True))]
     for call in bad:
         with pytest.raises(ValueError):
             call()

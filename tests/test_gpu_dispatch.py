@@ -153,28 +153,28 @@ def test_gradient_of_sort(T, k, E, S, cols, dt, kind):
     R.check(dx, want, off, "dx")
 
 
-def test_backward_leaves_the_rest_alone_without_its_number():
-    """The call itself: rows of grad_y behind the last are touched only where the number of rows is given; either result alone."""
+def test_backward_leaves_the_rest_alone_without_the_sources():
+    """The call itself: rows of grad_y that no entry names are touched only where the sources are given; either result alone."""
     from paper_2510_02613_amd import binding as B
     T, k, E, S, cols, dt = 33, 6, 64, 20, 520, BF16
     ids, m, row, y, w = made(T, k, E, S, cols, dt, "map")
-    offsets, _, _ = R.order(ids, S, m)
+    offsets, sources, _ = R.order(ids, S, m)
     total = int(offsets[-1])
     g = torch.randn(T, cols, generator=torch.Generator().manual_seed(9)).to(dt)
     dy, off_y, dw, off_w = R.backward(g, y, row, w)
-    dev = [t.cuda() for t in (g, y, row, w, offsets)]
-    for n_rows in (0, dev[4].data_ptr() + 4 * S):
+    dev = [t.cuda() for t in (g, y, row, w, sources)]
+    for source in (0, dev[4].data_ptr()):
         for wants in ((True, True), (True, False), (False, True)):
             gy = padded(torch.full((T * k, cols), 7.0, dtype=dt, device="cuda"), 3.0)
             gw = torch.full((T, k), 7.0, device="cuda")
             B.moe_combine_tokens_backward(B.MoECombineTokensBackward(
                 tokens=T, top_k=k, cols=cols, dtype=B.MOE_BF16, grad_out=dev[0].data_ptr(), ld_grad_out=cols, y=dev[1].data_ptr(), ld_y=cols, row=dev[2].data_ptr(),
-                weights=dev[3].data_ptr(), n_rows=n_rows, grad_y=gy.data_ptr() if wants[0] else 0, ld_grad_y=gy.stride(0), grad_weights=gw.data_ptr() if wants[1] else 0),
+                weights=dev[3].data_ptr(), source=source, grad_y=gy.data_ptr() if wants[0] else 0, ld_grad_y=gy.stride(0), grad_weights=gw.data_ptr() if wants[1] else 0),
                 torch.cuda.current_stream().cuda_stream)
             torch.cuda.synchronize()
             if wants[0]:
                 R.check(gy[:total], dy[:total], off_y[:total], "grad_y")
-                assert gy[total:].eq(0.0 if n_rows else 7.0).all() and gy.as_strided((T * k, 16), gy.stride(), cols).eq(3.0).all()
+                assert gy[total:].eq(0.0 if source else 7.0).all() and gy.as_strided((T * k, 16), gy.stride(), cols).eq(3.0).all()
             else:
                 assert gy.eq(7.0).all()
             if wants[1]:
@@ -227,6 +227,28 @@ def test_gradients_of_broadcast_and_shared_results():
         return torch.autograd.grad(D().combine_tokens(rows, order, w), x, grad)[0]
 
     assert torch.equal(dx_of(flat[1:].view(T, cols)), dx_of(flat[1:].view(T, cols).clone()))
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_dropped_assignments(dt):
+    """Entries of row that the caller sets to -1: nothing is added for them, and the gradient of their rows is zeros."""
+    T, k, E, S, cols = 70, 4, 16, 12, 264
+    ids, m, row, y, w = made(T, k, E, S, cols, dt, "map")
+    offsets, source, _ = R.order(ids, S, m)
+    for share in (0.3, 1.0):
+        kept = torch.where(torch.rand(T, k, generator=torch.Generator().manual_seed(3)) < share, -1, row).to(torch.int32)
+        order = D().Order(offsets.cuda(), source.cuda(), kept.cuda())
+        g = torch.randn(T, cols, generator=torch.Generator().manual_seed(9)).to(dt)
+        yg, wg = y.cuda().requires_grad_(), w.cuda().requires_grad_()
+        junk = [torch.full((T * k, cols), float("nan"), dtype=dt, device="cuda") for _ in range(4)]
+        del junk                                            # what the gradient may be allocated on
+        out = D().combine_tokens(yg, order, wg)
+        want, off = R.combine(y, kept, w)
+        R.check(out.detach(), want, off, "out")
+        got = torch.autograd.grad(out, (yg, wg), g.cuda())
+        dy, off_y, dw, off_w = R.backward(g, y, kept, w)
+        R.check(got[0], dy, off_y, "dy")
+        R.check(got[1], dw, off_w, "dweights")
 
 
 def test_a_gradient_of_a_gradient_is_refused():

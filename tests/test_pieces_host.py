@@ -77,6 +77,20 @@ def test_sorted_tokens_allocate_on_their_stream(monkeypatch, rec, call, side):
     assert [at for at, _ in rec.allocations] == [side] * n
 
 
+def test_given_results_of_products_count_as_changed(monkeypatch, rec):
+    from paper_2510_02613_amd import four_bit
+    Q = on_the_cpu(monkeypatch, rec, four_bit, "moe_four_bit_quantize", "moe_four_bit_matmul", "moe_four_bit_swiglu")
+    x, q, scale, out, half = z(4, 256, dt=BF16), z(4, 128), z(4, 8), z(4, 64, dt=BF16), z(4, 32, dt=BF16)
+    before = [t._version for t in (x, q, scale, out, half)]
+    Q.quantize(x, q=q, scale=scale, values=x)
+    Q.matmul(x, z(64, 128), z(64, 8), out=out)
+    Q.swiglu(x, z(64, 128), z(64, 8), out=half)
+    assert [t._version for t in (x, q, scale, out, half)] == [v + 1 for v in before]
+    with torch.inference_mode():
+        own = z(4, 64, dt=BF16)
+        assert Q.matmul(x, z(64, 128), z(64, 8), out=own) is own
+
+
 def test_given_results_count_as_changed(monkeypatch, rec):
     from paper_2510_02613_amd import dispatch
     D = on_the_cpu(monkeypatch, rec, dispatch, "moe_sort_tokens", "moe_combine_tokens")
