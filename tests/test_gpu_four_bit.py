@@ -147,7 +147,10 @@ def test_every_form_of_the_product(m, n, k):
 
 
 GROUP_FORMS = [([3] * 40, 2048, 768), ([3] * 40, 2048, 544), ([2, 3, 4, 0] * 10, 2048, 1312), ([3] * 40, 2048, 1536), ([20, 40, 0, 17] * 10, 1024, 512), ([20, 40, 0, 17] * 10, 1024, 1120),
-               ([1] + [0] * 70 + [5] + [0] * 200, 48, 160), ([0] * 500 + [2] + [0] * 300 + [1] + [0] * 99, 272, 96), ([0] * 1999 + [40], 16, 32), ([200] * 3 + [0] * 4 + [1000], 520, 96)]
+               ([1] + [0] * 70 + [5] + [0] * 200, 48, 160), ([0] * 500 + [2] + [0] * 300 + [1] + [0] * 99, 272, 96), ([0] * 1999 + [40], 16, 32), ([200] * 3 + [0] * 4 + [1000], 520, 96),
+               # several slices of weight rows with the same rows, one tile of them after the other; groups much longer than the others
+               ([20, 40, 0, 17] * 10, 4100, 288), ([12] * 38 + [0, 900], 1100, 736), ([12] * 38 + [0, 900], 2200, 768), ([2] * 39 + [150], 2100, 1024), ([2] * 39 + [150], 2100, 992),
+               ([1, 0] * 40, 2048, 512), ([1, 0] * 40, 2048, 544), ([20, 40, 0, 17] * 10, 1024, 1024), ([20, 40, 0, 17] * 10, 1024, 800)]
 
 
 @pytest.mark.parametrize("counts,n,k", GROUP_FORMS)
@@ -251,7 +254,8 @@ def test_every_form_of_swiglu(m, inter, k):
 
 
 @pytest.mark.parametrize("counts,inter,k", [([20, 40, 0, 17] * 10, 512, 544), ([20, 40, 0, 17] * 10, 512, 512), ([3] * 40, 1024, 4352), ([3] * 40, 1024, 4128), ([20, 40, 0, 17] * 5, 2048, 4128),
-                                            ([3] * 20, 640, 2048), ([0] * 500 + [2] + [0] * 399, 48, 96), ([1, 0, 0, 0] * 8, 2048, 4352)])
+                                            ([3] * 20, 640, 2048), ([0] * 500 + [2] + [0] * 399, 48, 96), ([1, 0, 0, 0] * 8, 2048, 4352),
+                                            ([20, 40, 0, 17] * 10, 1700, 288), ([20, 40, 0, 17] * 10, 1664, 2048), ([9] * 70, 1000, 96), ([12] * 38 + [0, 900], 2100, 1056)])
 def test_every_form_of_grouped_swiglu(counts, inter, k):
     groups, total = len(counts), sum(counts)
     a, q, s = case(k, total + 3, inter, k, groups)
