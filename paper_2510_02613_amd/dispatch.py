@@ -11,7 +11,8 @@ in place, and their rows behind the last one are not touched; results that a cal
 to `stream`.  Matrices are [rows, cols] with contiguous rows that start on 16 bytes; rows may lie further apart (`stride(0)`).
 
 Where grad mode is on and x, y or weights require gradients, they are computed by kernels of this library, on the stream that is current in the call;
-`stream` and results that are given are refused then, and so are gradients of gradients.
+`stream` and results that are given are refused then, and so are gradients of gradients.  A step that is captured into a graph together with its
+backward pass takes leaves that no eager graph still holds (torch keeps one accumulation node a leaf, on the stream of its first use).
 """
 from __future__ import annotations
 

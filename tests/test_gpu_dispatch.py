@@ -349,6 +349,31 @@ def test_two_streams_with_workspaces_of_their_own():
         assert torch.equal(o, D().combine_tokens(w.rows, w.order))
 
 
+def test_threads_with_gradients():
+    """Several threads at once, each on a stream of its own: x is copied k times, doubled and added up again."""
+    import threading
+    ids, _ = routing(2, 64, 8, 16, 16, "plain")
+    ids, wrong = ids.cuda(), []
+    torch.cuda.synchronize()
+
+    def steps():
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for n in range(1, 21):
+                x = torch.randn(64, 8 * n, device="cuda", requires_grad=True)
+                rows, order = D().sort_tokens(x, ids, 16)
+                D().combine_tokens(rows * 2, order).sum().backward()
+                if not x.grad.eq(16.0).all():
+                    wrong.append(n)
+
+    threads = [threading.Thread(target=steps) for _ in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong
+
+
 def test_rows_behind_2_to_the_32_bytes():
     """140000 assignments of 32 KB rows: the last ones lie past 2^32 bytes."""
     T, k, S, cols = 17500, 8, 3, 16384
