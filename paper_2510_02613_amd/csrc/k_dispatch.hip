@@ -124,8 +124,8 @@ enum { kCountAll, kAddUp, kScanned };     // where the counts of the assignments
 
 // A workgroup owns `per` tokens, at most 64 assignments, and every gridDim.y-th batch of `batch` runs of 64 16-byte columns of them: a wavefront has a batch of
 // a token's row on its way (the first from the start, while the assignments are counted) and writes it row by row.  A run at a time, each of another token
-// (and so of eight other rows): 71 us where this takes 66, 8192 tokens, 8 rows of 4 KB each, 4.6 TB/s.  Stores that are not kept in the caches: 81 -> 73 us by
-// themselves, but 117 -> 125 with the reader of the rows behind.
+// (and so of eight other rows): 5 us longer, 8192 tokens, 8 rows of 4 KB each, 302 MB, 63 us, 4.8 TB/s.  Stores that are not kept in the caches: 8 us less by
+// themselves, but 8 more with the reader of the rows behind.
 template <int kFrom>
 __global__ __launch_bounds__(kThreads) void k_sort_place(SortJob s, int per, int batch, int n_blocks)
 {
@@ -169,19 +169,34 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(SortJob s, int per, int
         behind.finish(first, s.n_groups);
     } else {
         if (kFrom == kAddUp) {
-            // a column of threads per group, as many rows of them as fit
-            int cols = 64;
-            while (cols < bins && cols < kThreads) cols *= 2;
-            const int b0 = tid / cols, step = kThreads / cols;
-            for (int g = tid & (cols - 1); g < bins; g += cols) {
-                int all = 0, before = 0;
-                for (int b = b0; b < n_blocks; b += step) {
-                    const int c = s.counts[(size_t)b * bins + g];
-                    all += c;
-                    before += b < block ? c : 0;
+            // all blocks' counts, four of a thread side by side and eight such on their way at once: other XCDs have just written them, a turn of waiting takes some 2 us
+            // (a thread a group and block after block: 75 us where this takes 63)
+            const int n = n_blocks * bins;
+            const auto add = [&](int b, int g, int c) __attribute__((always_inline)) {
+                if (c == 0) return;
+                atomicAdd(&first[g], c);
+                if (b < block) atomicAdd(&front[g], c);
+            };
+            constexpr int N = 8;
+            for (int i0 = tid; i0 < n / 4; i0 += N * kThreads) {
+                u32x4 c[N];
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+                    if (i0 + u * kThreads < n / 4) c[u] = *(const u32x4 *)(s.counts + (i0 + u * kThreads) * 4);
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    if (i0 + u * kThreads >= n / 4) break;
+                    int b = (i0 + u * kThreads) * 4 / bins, g = (i0 + u * kThreads) * 4 - b * bins;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        add(b, g, (int)c[u][e]);
+                        if (++g == bins) { g = 0; ++b; }
+                    }
                 }
-                if (all) atomicAdd(&first[g], all);
-                if (before) atomicAdd(&front[g], before);
+            }
+            if (tid < n % 4) {
+                const int at = n - n % 4 + tid;
+                add(at / bins, at % bins, s.counts[at]);
             }
         }
         Counter c;
