@@ -20,7 +20,6 @@ import functools
 from typing import NamedTuple, Optional
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as B
 from .layer import _owned_by
@@ -166,8 +165,33 @@ def _combine_backward(ctx, grad):
     return dy, dw, None, None
 
 
-# where a graph of the backward pass is asked for (create_graph), results that refuse a gradient of their own
-_sort_backward_once, _combine_backward_once = once_differentiable(_sort_backward), once_differentiable(_combine_backward)
+class _FirstOrder(torch.autograd.Function):
+    """A gradient in a graph of the backward pass (create_graph): it depends on `of`, and has no gradient of its own to them."""
+
+    @staticmethod
+    def forward(ctx, gradient, *of):
+        return gradient
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("sort_tokens and combine_tokens have no gradient of a gradient")
+
+
+# What each gradient depends on: dx on the rows' gradient; dy = w dout on the weights too, dw = <dout, y> on y too, also where dout is a constant
+def _sort_backward_graph(ctx, grad_rows):
+    with torch.no_grad():
+        dx, *rest = _sort_backward(ctx, grad_rows)
+    return dx if dx is None else _FirstOrder.apply(dx, grad_rows), *rest
+
+
+def _combine_backward_graph(ctx, grad):
+    with torch.no_grad():
+        dy, dw, *rest = _combine_backward(ctx, grad)
+    if grad is not None:
+        y, weights = ctx.saved_tensors
+        dy = dy if dy is None else _FirstOrder.apply(dy, grad, weights)
+        dw = dw if dw is None else _FirstOrder.apply(dw, grad, y)
+    return dy, dw, *rest
 
 
 class _SortTokens(torch.autograd.Function):
@@ -181,7 +205,7 @@ class _SortTokens(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_rows):
-        return (_sort_backward_once if torch.is_grad_enabled() else _sort_backward)(ctx, grad_rows)
+        return (_sort_backward_graph if torch.is_grad_enabled() else _sort_backward)(ctx, grad_rows)
 
 
 class _CombineTokens(torch.autograd.Function):
@@ -194,7 +218,7 @@ class _CombineTokens(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        return (_combine_backward_once if torch.is_grad_enabled() else _combine_backward)(ctx, grad)
+        return (_combine_backward_graph if torch.is_grad_enabled() else _combine_backward)(ctx, grad)
 
 
 def _refuse_given():
