@@ -98,3 +98,73 @@ def test_gradients_by_way_of_the_result_are_refused(weighted):
     dy, = torch.autograd.grad(D.combine_tokens(y, order, w if weighted else None).square().sum(), y, create_graph=True)
     with pytest.raises(RuntimeError):
         torch.autograd.grad(dy.sum(), y)
+
+
+# ---- derivatives in forward mode ----
+
+def four_bit(monkeypatch):
+    from paper_2510_02613_amd import four_bit as Q
+    monkeypatch.setattr(Q, "_device_of", lambda t: -1)
+    monkeypatch.setattr(Q, "_current_device", lambda: -1)
+    monkeypatch.setattr(Q, "_current_stream", lambda dev: 0)
+    for name in ("moe_four_bit_quantize", "moe_four_bit_matmul", "moe_four_bit_swiglu"):
+        monkeypatch.setattr(Q.B, name, lambda *a: None)
+    return Q
+
+
+def calls_of(Q):
+    """Calls by name, each of the tensor that its results depend on, and what to call them with."""
+    y, w, order, ids = inputs()
+    q, s = torch.zeros(64, 32, dtype=torch.uint8), torch.zeros(64, 2, dtype=torch.uint8)
+    half = torch.zeros(T, COLS, dtype=torch.bfloat16)
+    new = lambda rows, cols=COLS, dt=torch.float32: torch.zeros(rows, cols, dtype=dt)  # noqa: E731
+    return {
+        "sort": (lambda x: D.sort_tokens(x, ids, S).rows, new(T)),
+        "sort, given": (lambda x: D.sort_tokens(new(T), ids, S, rows=x).rows, new(T * K)),
+        "combine": (lambda x: D.combine_tokens(x, order, w), y),
+        "combine, weights": (lambda x: D.combine_tokens(y, order, x), w),
+        "combine, given": (lambda x: D.combine_tokens(y, order, w, out=x), new(T)),
+        "quantize": (lambda x: Q.quantize(x).q, new(T)),
+        "quantize, values": (lambda x: Q.quantize(new(T), values=x).q, new(T)),
+        "matmul": (lambda x: Q.matmul(x, q, s), half),
+        "matmul, addend": (lambda x: Q.matmul(half, q, s, add=x), new(T)),
+        "matmul, given": (lambda x: Q.matmul(half, q, s, out=x), new(T)),
+        "swiglu": (lambda x: Q.swiglu(x, q, s), half),
+        "swiglu, given": (lambda x: Q.swiglu(half, q, s, out=x), new(T, 32)),
+    }
+
+
+CALLS = ["sort", "sort, given", "combine", "combine, weights", "combine, given", "quantize", "quantize, values", "matmul", "matmul, addend", "matmul, given", "swiglu",
+         "swiglu, given"]
+
+
+@pytest.mark.parametrize("no_grad", [False, True])
+@pytest.mark.parametrize("name", CALLS)
+def test_derivatives_in_forward_mode_are_refused(monkeypatch, name, no_grad):
+    """A dual number's derivative would be missing from the result, with no error; torch.no_grad() does not turn this mode off."""
+    f, x = calls_of(four_bit(monkeypatch))[name]
+    f(x)
+    with torch.autograd.forward_ad.dual_level(), torch.set_grad_enabled(not no_grad):
+        f(x)                                        # only tensors that carry one
+        with pytest.raises(ValueError, match="forward"):
+            f(torch.autograd.forward_ad.make_dual(x, torch.ones_like(x)))
+    f(x)
+
+
+@pytest.mark.parametrize("of", ["sort", "combine"])
+def test_derivatives_in_forward_mode_of_gradients_are_refused(of):
+    y, w, order, ids = inputs()
+    leaf = torch.zeros(T, COLS, requires_grad=True) if of == "sort" else y.requires_grad_()
+    out = D.sort_tokens(leaf, ids, S).rows if of == "sort" else D.combine_tokens(leaf, order, w)
+    with torch.autograd.forward_ad.dual_level():
+        grad = torch.autograd.forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out))
+        with pytest.raises(ValueError, match="forward"):
+            torch.autograd.grad(out, leaf, grad, retain_graph=True)
+        torch.autograd.grad(out, leaf, torch.ones_like(out))
+
+
+def test_tensors_of_other_types_are_refused_as_ever():
+    with torch.autograd.forward_ad.dual_level():
+        for dt in (torch.int32, torch.float16):
+            with pytest.raises(ValueError, match="x must be"):
+                D.sort_tokens(torch.zeros(T, COLS, dtype=dt), torch.zeros(T, K, dtype=torch.int32), S)
