@@ -1,7 +1,11 @@
-"""Derivatives that torch would lose without a word: its forward mode sees neither the kernels nor that a result which a call makes or is given depends on its arguments."""
+"""What torch would lose without a word: it sees neither the kernels nor that a result which a call makes or is given depends on its arguments.  Its forward mode
+would leave a derivative out, a trace would hold the result's allocation and no call."""
 from __future__ import annotations
 
+import torch
 from torch.autograd import forward_ad
+
+_is_tracing, _count_modes = torch._C._is_tracing, torch._C._len_torch_dispatch_stack
 
 
 def forward_mode() -> bool:
@@ -14,3 +18,9 @@ def refuse_duals(*tensors) -> None:
     for t in tensors:
         if t is not None and forward_ad.unpack_dual(t).tangent is not None:
             raise ValueError("there is no derivative in forward mode: call with the primal tensor")
+
+
+def refuse_traces() -> None:
+    """Of torch.jit.trace and of make_fx on tensors with values.  Without such values (export, compilation) the tensors have no address, which torch refuses."""
+    if _is_tracing() or (_count_modes() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None):
+        raise ValueError("the library's calls cannot be traced: a trace would hold their results' allocation only")

@@ -11,7 +11,7 @@ in place, and their rows behind the last one are not touched; results that a cal
 to `stream`.  Matrices are [rows, cols] with contiguous rows that start on 16 bytes; rows may lie further apart (`stride(0)`).
 
 Where grad mode is on and x, y or weights require gradients, they are computed by kernels of this library, on the stream that is current in the call;
-`stream` and results that are given are refused then, and so are gradients of gradients; derivatives in forward mode are refused always.  A step that is captured into a graph together with its
+`stream` and results that are given are refused then, and so are gradients of gradients; derivatives in forward mode and traces are refused always.  A step that is captured into a graph together with its
 backward pass takes leaves that no eager graph still holds (torch keeps one accumulation node a leaf, on the stream of its first use).
 """
 from __future__ import annotations
@@ -22,7 +22,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as B
-from .derivatives import forward_mode, refuse_duals
+from .derivatives import forward_mode, refuse_duals, refuse_traces
 from .layer import _owned_by
 from .scaled import _DTYPE, _current_device, _current_stream, _device_of, _matrix, _whole
 
@@ -242,6 +242,7 @@ def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map
     if dev != _current_device():
         with torch.cuda.device(dev):
             return sort_tokens(x, ids, n_groups, expert_map=expert_map, rows=rows, order=order, workspace=workspace, stream=stream)
+    refuse_traces()
     if forward_mode():
         refuse_duals(x, rows)
     if x.requires_grad and torch.is_grad_enabled():
@@ -264,6 +265,7 @@ def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor
     if dev != _current_device():
         with torch.cuda.device(dev):
             return combine_tokens(y, order, weights, out=out, stream=stream)
+    refuse_traces()
     if forward_mode():
         refuse_duals(y, weights, out)
     if (y.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():

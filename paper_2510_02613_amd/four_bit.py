@@ -7,7 +7,7 @@ are contiguous, [n, k / 2] or, for sorted rows, [groups, n, k / 2], their powers
 that name them, torch.float4_e2m1fn_x2 and torch.float8_e8m0fnu.
 
 The products are for serving: they have no gradient, and refuse tensors that ask for one while grad mode is on, and those that carry a
-derivative in forward mode.
+derivative in forward mode; and they refuse to be traced.
 """
 from __future__ import annotations
 
@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as B
-from .derivatives import forward_mode, refuse_duals
+from .derivatives import forward_mode, refuse_duals, refuse_traces
 from .layer import _owned_by
 from .scaled import _DTYPE, _current_device, _current_stream, _device_of, _matrix, _whole
 
@@ -55,6 +55,7 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
     if dev != _current_device():      # kernels run on the tensors' device, whichever is current
         with torch.cuda.device(dev):
             return quantize(x, q=q, scale=scale, values=values, stream=stream)
+    refuse_traces()
     if forward_mode():
         refuse_duals(x, values)
     if torch.is_grad_enabled() and (x.requires_grad or (values is not None and values.requires_grad)):
@@ -108,6 +109,7 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return matmul(a, w, w_scale, offsets=offsets, add=add, out=out, out_dtype=out_dtype, stream=stream)
+    refuse_traces()
     if forward_mode():
         refuse_duals(a, add, out)
     if torch.is_grad_enabled() and (a.requires_grad or (add is not None and add.requires_grad) or (out is not None and out.requires_grad)):
@@ -137,6 +139,7 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return swiglu(a, w, w_scale, offsets=offsets, out=out, out_dtype=out_dtype, stream=stream)
+    refuse_traces()
     if forward_mode():
         refuse_duals(a, out)
     if torch.is_grad_enabled() and (a.requires_grad or (out is not None and out.requires_grad)):

@@ -168,3 +168,24 @@ def test_tensors_of_other_types_are_refused_as_ever():
         for dt in (torch.int32, torch.float16):
             with pytest.raises(ValueError, match="x must be"):
                 D.sort_tokens(torch.zeros(T, COLS, dtype=dt), torch.zeros(T, K, dtype=torch.int32), S)
+
+
+# ---- traces ----
+
+@pytest.mark.parametrize("name", CALLS)
+def test_traces_are_refused(monkeypatch, name):
+    """What is traced would hold the allocation of the result and no call."""
+    from torch.fx.experimental.proxy_tensor import make_fx
+    f, x = calls_of(four_bit(monkeypatch))[name]
+    with pytest.raises(ValueError, match="trace"):
+        torch.jit.trace(f, (x,), check_trace=False)
+    with pytest.raises(ValueError, match="trace"):
+        make_fx(f)(x)
+    f(x)
+
+
+def test_other_modes_of_torch_are_not_in_the_way(monkeypatch):
+    from torch.utils.flop_counter import FlopCounterMode
+    with FlopCounterMode(display=False):
+        for f, x in calls_of(four_bit(monkeypatch)).values():
+            f(x)
