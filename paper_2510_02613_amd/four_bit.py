@@ -44,8 +44,10 @@ def _named(t: torch.Tensor, dtypes):
 _increment_version = torch.autograd.graph.increment_version
 
 
-def _refuse_gradient():
-    raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
+def _refuse_gradients(*tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
 
 
 def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None,
@@ -57,9 +59,9 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
             return quantize(x, q=q, scale=scale, values=values, stream=stream)
     refuse_traces()
     if forward_mode():
-        refuse_duals(x, values)
-    if torch.is_grad_enabled() and (x.requires_grad or (values is not None and values.requires_grad)):
-        _refuse_gradient()
+        refuse_duals(x, q, scale, values)
+    if torch.is_grad_enabled():
+        _refuse_gradients(x, q, scale, values)
     if x.dim() != 2 or x.dtype not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
     rows, cols = x.shape
@@ -111,9 +113,9 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
             return matmul(a, w, w_scale, offsets=offsets, add=add, out=out, out_dtype=out_dtype, stream=stream)
     refuse_traces()
     if forward_mode():
-        refuse_duals(a, add, out)
-    if torch.is_grad_enabled() and (a.requires_grad or (add is not None and add.requires_grad) or (out is not None and out.requires_grad)):
-        _refuse_gradient()
+        refuse_duals(a, w, w_scale, add, out)
+    if torch.is_grad_enabled():
+        _refuse_gradients(a, w, w_scale, add, out)
     m, k = a.shape
     groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
     given = out is not None
@@ -141,9 +143,9 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
             return swiglu(a, w, w_scale, offsets=offsets, out=out, out_dtype=out_dtype, stream=stream)
     refuse_traces()
     if forward_mode():
-        refuse_duals(a, out)
-    if torch.is_grad_enabled() and (a.requires_grad or (out is not None and out.requires_grad)):
-        _refuse_gradient()
+        refuse_duals(a, w, w_scale, out)
+    if torch.is_grad_enabled():
+        _refuse_gradients(a, w, w_scale, out)
     m, k = a.shape
     groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
     if n % 2:

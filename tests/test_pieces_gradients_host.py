@@ -189,3 +189,20 @@ def test_other_modes_of_torch_are_not_in_the_way(monkeypatch):
     with FlopCounterMode(display=False):
         for f, x in calls_of(four_bit(monkeypatch)).values():
             f(x)
+
+
+# ---- powers whose type could have a gradient ----
+
+@pytest.mark.parametrize("which", ["scale", "w_scale"])
+def test_powers_that_ask_for_a_gradient_are_refused(monkeypatch, which):
+    Q = four_bit(monkeypatch)
+    powers = torch.zeros(64, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    x = torch.zeros(64, 64, dtype=torch.bfloat16)
+    call = {"scale": lambda p: Q.quantize(x, scale=p), "w_scale": lambda p: Q.matmul(x, torch.zeros(64, 32, dtype=torch.uint8), p)}[which]
+    with torch.autograd.forward_ad.dual_level(), pytest.raises(ValueError, match="forward"):
+        call(torch.autograd.forward_ad.make_dual(powers, powers.clone()))
+    powers.requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        call(powers)
+    with torch.no_grad():
+        call(powers)
