@@ -136,14 +136,24 @@ def _rows16(t: torch.Tensor) -> torch.Tensor:
 
 def _unchanged(t: torch.Tensor, version: int) -> None:
     if t._version != version:
-        raise RuntimeError("the order of the tokens was overwritten since the call whose gradient is wanted: its buffers were given to another call")
+        raise RuntimeError("the order of the tokens was changed in place since the call whose gradient is wanted, by the caller or by a call that its buffers were given to")
+
+
+def _places(source: torch.Tensor, routing) -> torch.Tensor:
+    """row of an Order, from its source: places behind the last one have a spare entry each, so that no two write to one."""
+    A = source.numel()
+    at = torch.arange(A, dtype=torch.int64, device=source.device)
+    places = torch.full((2 * A,), -1, dtype=torch.int32, device=source.device)
+    return places.scatter_(0, torch.where(source >= 0, source, at + A), at.int())[:A].view(routing)
 
 
 def _sort_backward(ctx, grad_rows):
     if grad_rows is None:
         return None, None, None, None, None, None
-    row, version = ctx.row
-    _unchanged(row, version)
+    source, row, *versions = ctx.order
+    if row._version != versions[1]:                     # entries were set to -1: what combine_tokens drops, the rows' gradient may still have from elsewhere
+        _unchanged(source, versions[0])
+        row = _places(source, row.shape)
     return _combine(_rows16(grad_rows), row, None, None, None, grad_rows.get_device()), None, None, None, None, None
 
 
@@ -203,7 +213,7 @@ class _SortTokens(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         rows = torch.empty((ids.numel(), x.shape[1]), dtype=x.dtype, device=x.device)
         _sort(x, ids, n_groups, expert_map, rows, order, workspace, None, x.get_device(), zero_rest=True)
-        ctx.row = order.row, order.row._version
+        ctx.order = order.source, order.row, order.source._version, order.row._version
         return rows
 
     @staticmethod
@@ -260,7 +270,7 @@ def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map
 def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """out[t] = sum over j of weights[t, j] * y[order.row[t, j]], of the assignments that have a row; weights float32 [tokens, top_k], None: ones.
-    Entries of order.row may be set to -1 (assignments that are dropped); rows that none names have a gradient of zeros."""
+    Entries of order.row may be set to -1 before (assignments that are dropped), in place or in another Order; rows that none names have a gradient of zeros."""
     dev = _device_of(y)
     if dev != _current_device():
         with torch.cuda.device(dev):

@@ -206,3 +206,58 @@ def test_powers_that_ask_for_a_gradient_are_refused(monkeypatch, which):
         call(powers)
     with torch.no_grad():
         call(powers)
+
+
+# ---- assignments that are dropped between the sort and the combination ----
+
+def dropping_step(x, w, ids, drop, how):
+    """(out, rows) of x with assignments dropped, by torch's own operations where `how` is "plain"."""
+    if how == "plain":
+        rows = x[:, None].expand(T, K, COLS)
+        kept = torch.where((ids >= 0) & (ids < S) & ~drop, w, torch.zeros(()))
+        return (kept[..., None] * (2 * rows)).sum(1), torch.where(((ids >= 0) & (ids < S))[..., None], rows, 0.0)
+    rows, order = D.sort_tokens(x, ids, S)
+    if how == "in place":
+        order.row[drop] = -1
+    else:
+        order = order._replace(row=order.row.masked_fill(drop, -1))
+    return D.combine_tokens(2 * rows, order, w), rows
+
+
+@pytest.mark.parametrize("how", ["in place", "copy"])
+def test_assignments_dropped_after_the_sort(how):
+    """Gradients of tokens and weights through sort, drop and combine; rows that are used elsewhere too keep that part of their gradient, dropped or not."""
+    _, w, _, ids = inputs()
+    x, drop = torch.randn(T, COLS), torch.tensor([[True, False], [False, False], [True, True], [False, True]])
+    grad, more = torch.randn(T, COLS), torch.randn(COLS)
+    got, want = [], []
+    for to, h in ((got, how), (want, "plain")):
+        xs, ws = x.clone().requires_grad_(), w.clone().requires_grad_()
+        out, rows = dropping_step(xs, ws, ids, drop, h)
+        to.extend((out.detach(), *torch.autograd.grad((out * grad).sum() + (rows * more).sum(), (xs, ws))))
+    for a, b in zip(got, want):
+        assert torch.allclose(a, b, rtol=1e-5, atol=1e-5)
+
+
+def test_what_else_is_changed_after_the_sort_is_refused():
+    """The rows' assignments tell the sort where its rows came from: with them gone it has no gradient, and says so.  So has the combination when its entries change behind it."""
+    _, w, _, ids = inputs()
+    x = torch.randn(T, COLS, requires_grad=True)
+    rows, order = D.sort_tokens(x, ids, S)
+    order.row[0] = -1
+    order.source[0] = -1
+    with pytest.raises(RuntimeError, match="changed in place"):
+        torch.autograd.grad(rows.sum(), x)
+    rows, order = D.sort_tokens(x, ids, S)
+    out = D.combine_tokens(rows, order, w)
+    order.row[0] = -1
+    with pytest.raises(RuntimeError, match="changed in place"):
+        torch.autograd.grad(out.sum(), x)
+
+
+@pytest.mark.parametrize("tokens,k,n_groups", [(0, 2, 3), (1, 1, 1), (7, 3, 4), (40, 8, 5)])
+def test_places_from_the_rows_assignments(tokens, k, n_groups):
+    ids = torch.randint(-1, n_groups + 2, (tokens, k), generator=torch.Generator().manual_seed(tokens), dtype=torch.int32)
+    _, source, row = R.order(ids, n_groups)
+    got = D._places(source, ids.shape)
+    assert got.dtype == torch.int32 and got.is_contiguous() and torch.equal(got, row)
