@@ -15,7 +15,8 @@ extern "C" {
  * A 4-bit matrix [rows, cols], cols a multiple of 32, is two e2m1 values a byte -- 0, 0.5, 1, 1.5, 2, 3, 4, 6, the sign in bit 3; the even column in
  * bits 0..3 -- and an e8m0 byte b, the power of two 2^(b - 127), for each row and 32 consecutive columns; b = 255 makes its 32 values NaN.
  * Quantising takes the smallest power of two (2^-127 at least) that leaves no magnitude of the 32 above 6, and v / 2^p to the nearest, ties to the even
- * code; signs are kept, of zeros too.  A group that holds a NaN or an infinity gets b = 255 and zeros.
+ * code; signs are kept, of zeros too.  A group that holds a NaN or an infinity gets b = 255 and zeros.  Powers of 2^126 and 2^127 reach values of 2^128 and
+above, which are infinities in fp32 and bf16: as quantised values, where magnitudes from 3.5 * 2^126 (2.98e38) on get 2^128, and as the weights of a product.
  * Strides (ld) count elements from one row to the next, bytes for q and scale; rows behind the last one are not touched.  All pointers are device pointers,
  * nothing is allocated or synchronised, rows == 0 and m == 0 are no-ops.  Unless a call says otherwise its outputs must not overlap each other or its inputs.
  */
@@ -41,7 +42,7 @@ moe_status_t moe_four_bit_quantize(const moe_four_bit_quantize_t *args, void *hi
 /*
  * out = a w^T (+ add): bf16 rows times 4-bit weights.  With offsets (device, as moe_sort_tokens writes them) row r of group g, offsets[g] <= r <
  * offsets[g + 1], takes the weights w[g]; rows in no group are not touched, and what offsets name outside [0, m) is left out.  Offsets must not decrease.
- * A weight times its power of two is a bf16 number, so that products are exact; their sums are fp32's, rounded once at the end.  The order of a sum
+ * A weight times its power of two is a bf16 number (below 2^128), so that products are exact; their sums are fp32's, rounded once at the end.  The order of a sum
  * depends on the sizes of the call, not on what runs beside it.  out may be add itself (same address and ld).
  * Made for few rows a group, where the weights' bytes are what a product costs; many rows work too, at about half the rate of a bf16 product.
  *   MOE_ERR_UNSUPPORTED: k no multiple of 32; m, n or k > 2^21; ld_a >= 2^24; groups > 2047; more tiles than a launch can have workgroups.

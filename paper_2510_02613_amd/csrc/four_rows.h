@@ -2,8 +2,8 @@
 //
 //   out[r, c] = sum_k a[r, k] code[c, k] 2^p[c, k / 32]
 //
-// A code times its power of two is a bf16 number (2^-128 .. 6 * 2^126 and its infinities): the conversion instruction makes two of them from a byte and the
-// power, the products are exact and the sums fp32's.
+// A code times its power of two is a bf16 number, 2^-128 .. 1.5 * 2^127 in magnitude, and infinite from 2^128 on (powers 2^126 and 2^127 alone): the conversion
+// instruction makes two of them from a byte and the power, the products are exact and the sums fp32's.
 // A K-step is a line of a weight row, 128 bytes or 256 columns, in two halves: of half h lane (quad, l15) has the 16 bytes of row l15 that hold the columns
 // 128 h + 32 quad .. + 31, one group with one power, and instruction i takes the eight from 8 i, of the activation row the same.  Which k an instruction pairs
 // with which does not matter: both sides agree.  Weight rows are the first operand, so that a lane holds neighbouring columns of one row of the result:
