@@ -57,7 +57,7 @@ moe_status_t moe_sort_tokens(const moe_sort_tokens_t *args, void *hip_stream);
 /*
  * out[t] = sum over j of weights[t, j] * y[row[t, j]], in the order of j, assignments without a row left out: added up in fp32, rounded once.
  * weights NULL: ones, which is the gradient of moe_sort_tokens (y: the rows' gradient, out: the tokens').  A token without rows gets zeros.
- * An entry of row outside [0, tokens * top_k) has no row; weights and rows that no entry names are not read.
+ * An entry of row outside [0, tokens * top_k) has no row, and its weight does not count, whatever it is; rows that no entry names are not read.
  */
 typedef struct {
     int32_t tokens, top_k, cols;

@@ -23,7 +23,7 @@ struct FourGemm {
     const uint8_t *w, *ws;
     int32_t m, n, k, groups;
     const int32_t *offsets;               // NULL: all rows are group 0's
-    int32_t sparse;                       // many groups may have no rows
+    int32_t sparse;                       // more groups than twice the rows: many have none
     const void *add;
     int64_t ld_add;
     void *out;

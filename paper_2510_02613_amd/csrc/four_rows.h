@@ -27,7 +27,7 @@ constexpr int kLine = 256;                // columns of a line of a weight row
 constexpr int kPowers = 72;               // bytes in LDS from one weight row's powers to the next: 64 of them and a gap against bank conflicts
 constexpr size_t kMostLds = 160 * 1024;
 
-// The n-th group (lo, hi: its rows), -1 if it has none; where there are more groups than half the rows (sparse) the n-th that has some: every workgroup looks for
+// The n-th group (lo, hi: its rows), -1 if it has none; where there are more groups than twice the rows (sparse) the n-th that has some: every workgroup looks for
 // itself, and groups without rows cost none then.
 __device__ __forceinline__ int nth_group(const FourGemm &g, int n, int &lo, int &hi)
 {

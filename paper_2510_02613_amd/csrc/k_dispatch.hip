@@ -95,7 +95,8 @@ __device__ __forceinline__ void scan_groups(int32_t *total, const int32_t *more,
 }
 
 // One block's counts -> the place of its first assignment of every group: many assignments (more than the workgroups of k_sort_place add up
-// themselves), one workgroup.
+// themselves), one workgroup, block after block.  Bound by the latency of its loads: 65536 tokens, 8 rows of 4 KB each, 128 groups, 652 us for the sort, where
+// adding up takes 515; 8 times the 59 us of 8192 tokens would be 475.
 __global__ __launch_bounds__(kThreads) void k_sort_scan(SortJob s, int n_blocks)
 {
     extern __shared__ int32_t total[];    // [n_groups + 1]
@@ -379,7 +380,10 @@ hipError_t launch_sort_tokens(const SortJob &j, hipStream_t st)
     const int bins = j.n_groups + 1, n_blocks = sort_blocks(j.tokens, j.top_k);
     int per = 64 / j.top_k;
     const int runs = (j.chunks + 63) / 64;
-    // few tokens: fewer of them to a workgroup, then shorter batches on more workgroups
+    // few tokens: fewer of them to a workgroup, then shorter batches on more workgroups.  us (a quarter of the limit, four times as much), 8 assignments a token, 128 groups:
+    //   512 workgroups: 2048 tokens of 256 columns 11.1 (11.1, 15.3), 8192 20.1 (20.1, 24.3), 2048 of 7168 52 (54, 49), 512 of 256 8.3 (7.6, 8.3)
+    //   4096 batches: 8192 tokens of 2048 columns 59.7 (59.3, 66.0), 2048 of 7168 50.6 (51.3, 57.5), 256 of 7168 11.2 (10.1, 11.1)
+    //   512 workgroups in all: 128 tokens of 7168 columns 8.1 (11.5, 8.1), 64 6.6 (7.9, 6.5), 512 17.9 (17.9, 19.0)
     while (per > 1 && (j.tokens + per - 1) / per < 512) per = (per + 1) / 2;
     const int gx = j.tokens > 0 ? (j.tokens + per - 1) / per : 1;
     int batch = 4;
