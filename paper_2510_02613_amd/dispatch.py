@@ -22,7 +22,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as B
-from .derivatives import forward_mode, refuse_duals, refuse_traces
+from .derivatives import refuse_duals, refuse_watched, watched
 from .layer import _owned_by
 from .scaled import _DTYPE, _current_device, _current_stream, _device_of, _matrix, _whole
 
@@ -43,7 +43,7 @@ class Sorted(NamedTuple):
 _pack_sort, _pack_combine = B.packer(B.MoESortTokens), B.packer(B.MoECombineTokens)
 _pack_backward = B.packer(B.MoECombineTokensBackward)
 # results that were given count as changed in place: a backward pass that was to read what they held refuses
-_increment_version = torch.autograd.graph.increment_version
+_increment_version, _grad_enabled = torch._C._increment_version, torch.is_grad_enabled
 
 
 _workspace_bytes = functools.lru_cache(maxsize=1024)(B.moe_sort_tokens_workspace_bytes)      # of sizes alone
@@ -81,7 +81,7 @@ def _sort(x, ids, n_groups, expert_map, rows, order, workspace, stream, dev, zer
         pm = _whole(expert_map, expert_map.shape, torch.int32, dev, "expert_map")
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("the workspace must be contiguous and on the device of x")
-    written = [t for t in (rows, *(order or ())) if t is not None]
+    written = (rows, *order) if rows is not None and order is not None else order or (() if rows is None else (rows,))
     if rows is None or order is None or (workspace is None and _workspace_bytes(tokens, top_k, n_groups)):
         with _owned_by(stream):
             if rows is None:
@@ -122,13 +122,13 @@ def _combine(y, row, weights, out, stream, dev):
     B.moe_combine_tokens(_pack_combine(tokens, top_k, cols, _DTYPE[dt], py, ld_y, pr, pw, po, ld_o),
                          _current_stream(dev) if stream is None else stream.cuda_stream)
     if given:
-        _increment_version(out)
+        _increment_version((out,))
     return out
 
 
 def _rows16(t: torch.Tensor) -> torch.Tensor:
     """A gradient as the kernels read it: autograd's may be broadcast or start anywhere."""
-    if forward_mode():
+    if watched():
         refuse_duals(t)
     t = t.contiguous()
     return t if t.data_ptr() % 16 == 0 else t.clone()
@@ -239,7 +239,7 @@ def _refuse_given():
 
 
 def _refuse_leaf(given):
-    if given.requires_grad and torch.is_grad_enabled():
+    if given.requires_grad and _grad_enabled():
         raise ValueError("results that are given must not require a gradient")
 
 
@@ -252,10 +252,9 @@ def sort_tokens(x: torch.Tensor, ids: torch.Tensor, n_groups: int, *, expert_map
     if dev != _current_device():
         with torch.cuda.device(dev):
             return sort_tokens(x, ids, n_groups, expert_map=expert_map, rows=rows, order=order, workspace=workspace, stream=stream)
-    refuse_traces()
-    if forward_mode():
-        refuse_duals(x, rows)
-    if x.requires_grad and torch.is_grad_enabled():
+    if watched():
+        refuse_watched(x, rows)
+    if x.requires_grad and _grad_enabled():
         if rows is not None or order is not None or stream is not None:
             _refuse_given()
         if ids.dim() != 2 or n_groups <= 0 or x.dim() != 2:
@@ -275,10 +274,9 @@ def combine_tokens(y: torch.Tensor, order: Order, weights: Optional[torch.Tensor
     if dev != _current_device():
         with torch.cuda.device(dev):
             return combine_tokens(y, order, weights, out=out, stream=stream)
-    refuse_traces()
-    if forward_mode():
-        refuse_duals(y, weights, out)
-    if (y.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
+    if watched():
+        refuse_watched(y, weights, out)
+    if (y.requires_grad or (weights is not None and weights.requires_grad)) and _grad_enabled():
         if out is not None or stream is not None:
             _refuse_given()
         if order.source is None:

@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as B
-from .derivatives import forward_mode, refuse_duals, refuse_traces
+from .derivatives import any_requires_grad, refuse_watched, watched
 from .layer import _owned_by
 from .scaled import _DTYPE, _current_device, _current_stream, _device_of, _matrix, _whole
 
@@ -41,13 +41,11 @@ def _named(t: torch.Tensor, dtypes):
 
 
 # results that were given count as changed in place
-_increment_version = torch.autograd.graph.increment_version
+_increment_version, _grad_enabled = torch._C._increment_version, torch.is_grad_enabled
 
 
-def _refuse_gradients(*tensors):
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
+def _refuse_gradient():
+    raise ValueError("4-bit operators have no gradient: call them under torch.no_grad()")
 
 
 def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None,
@@ -57,24 +55,25 @@ def quantize(x: torch.Tensor, *, q: Optional[torch.Tensor] = None, scale: Option
     if dev != _current_device():      # kernels run on the tensors' device, whichever is current
         with torch.cuda.device(dev):
             return quantize(x, q=q, scale=scale, values=values, stream=stream)
-    refuse_traces()
-    if forward_mode():
-        refuse_duals(x, q, scale, values)
-    if torch.is_grad_enabled():
-        _refuse_gradients(x, q, scale, values)
-    if x.dim() != 2 or x.dtype not in _DTYPE:
+    if watched():
+        refuse_watched(x, q, scale, values)
+    if _grad_enabled() and any_requires_grad(x, q, scale, values):
+        _refuse_gradient()
+    shape, dt = x.shape, x.dtype
+    if len(shape) != 2 or dt not in _DTYPE:
         raise ValueError("x must be a bfloat16 or float32 matrix")
-    rows, cols = x.shape
-    written = [t for t in (q, scale, values) if t is not None]
+    rows, cols = shape
+    written = (q, scale) if values is None else (q, scale, values)
     if q is None or scale is None:
+        written = [t for t in written if t is not None]
         with _owned_by(stream):
             q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device) if q is None else q
             scale = torch.empty((rows, cols // GROUP), dtype=torch.uint8, device=x.device) if scale is None else scale
-    px, ld_x = _matrix(x, (rows, cols), x.dtype, dev, "x")
+    px, ld_x = _matrix(x, shape, dt, dev, "x")
     pq, ld_q = _matrix(q, (rows, cols // 2), _named(q, _CODES), dev, "q")
     ps, ld_s = _matrix(scale, (rows, cols // GROUP), _named(scale, _POWERS), dev, "scale")
-    pv, ld_v = (0, 0) if values is None else _matrix(values, (rows, cols), x.dtype, dev, "values")
-    B.moe_four_bit_quantize(_pack_quantize(rows, cols, _DTYPE[x.dtype], px, ld_x, pq, ld_q, ps, ld_s, pv, ld_v),
+    pv, ld_v = (0, 0) if values is None else _matrix(values, shape, dt, dev, "values")
+    B.moe_four_bit_quantize(_pack_quantize(rows, cols, _DTYPE[dt], px, ld_x, pq, ld_q, ps, ld_s, pv, ld_v),
                             _current_stream(dev) if stream is None else stream.cuda_stream)
     if written:
         _increment_version(written)
@@ -86,15 +85,13 @@ def _weights(w, w_scale, offsets, k, dev):
     if offsets is None:
         if w.dim() != 2:
             raise ValueError("w must be [n, k / 2] without offsets")
-        n, = lead = w.shape[:1]
-        groups, po = 1, 0
-    else:
-        if w.dim() != 3:
-            raise ValueError("w must be [groups, n, k / 2] with offsets")
-        groups, n = lead = w.shape[:2]
-        po = _whole(offsets, (groups + 1,), torch.int32, dev, "offsets")
-    return (groups, n, po, _whole(w, (*lead, k // 2), _named(w, _CODES), dev, "w"),
-            _whole(w_scale, (*lead, k // GROUP), _named(w_scale, _POWERS), dev, "w_scale"))
+        n = w.shape[0]
+        return (1, n, 0, _whole(w, (n, k // 2), _named(w, _CODES), dev, "w"), _whole(w_scale, (n, k // GROUP), _named(w_scale, _POWERS), dev, "w_scale"))
+    if w.dim() != 3:
+        raise ValueError("w must be [groups, n, k / 2] with offsets")
+    groups, n, _ = w.shape
+    return (groups, n, _whole(offsets, (groups + 1,), torch.int32, dev, "offsets"), _whole(w, (groups, n, k // 2), _named(w, _CODES), dev, "w"),
+            _whole(w_scale, (groups, n, k // GROUP), _named(w_scale, _POWERS), dev, "w_scale"))
 
 
 def _result(m, cols, dtype, device, offsets, stream):
@@ -111,11 +108,10 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return matmul(a, w, w_scale, offsets=offsets, add=add, out=out, out_dtype=out_dtype, stream=stream)
-    refuse_traces()
-    if forward_mode():
-        refuse_duals(a, w, w_scale, add, out)
-    if torch.is_grad_enabled():
-        _refuse_gradients(a, w, w_scale, add, out)
+    if watched():
+        refuse_watched(a, w, w_scale, add, out)
+    if _grad_enabled() and any_requires_grad(a, w, w_scale, add, out):
+        _refuse_gradient()
     m, k = a.shape
     groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
     given = out is not None
@@ -130,7 +126,7 @@ def matmul(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     B.moe_four_bit_matmul(_pack_matmul(m, n, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pd, ld_d, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
     if given:
-        _increment_version(out)
+        _increment_version((out,))
     return out
 
 
@@ -141,11 +137,10 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     if dev != _current_device():
         with torch.cuda.device(dev):
             return swiglu(a, w, w_scale, offsets=offsets, out=out, out_dtype=out_dtype, stream=stream)
-    refuse_traces()
-    if forward_mode():
-        refuse_duals(a, w, w_scale, out)
-    if torch.is_grad_enabled():
-        _refuse_gradients(a, w, w_scale, out)
+    if watched():
+        refuse_watched(a, w, w_scale, out)
+    if _grad_enabled() and any_requires_grad(a, w, w_scale, out):
+        _refuse_gradient()
     m, k = a.shape
     groups, n, po, pw, ps = _weights(w, w_scale, offsets, k, dev)
     if n % 2:
@@ -162,5 +157,5 @@ def swiglu(a: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, offsets: 
     B.moe_four_bit_swiglu(_pack_swiglu(m, inter, k, groups, _DTYPE[dt], pa, ld_a, po, pw, ps, pt, ld_t),
                           _current_stream(dev) if stream is None else stream.cuda_stream)
     if given:
-        _increment_version(out)
+        _increment_version((out,))
     return out
